@@ -14,6 +14,10 @@
  *   d3tom_proj_qkv          (supporting) Q,K,V projection of a post-merge layer
  *   d3tom_linear, d3tom_ffn (supporting) output projection and gated feed-forward
  *                           network of a post-merge block
+ *   d3tom_rope              (supporting) rotary positions with up to three axes
+ *   d3tom_cache_append, d3tom_attn_cached, d3tom_cache_evict
+ *                           (supporting) a K/V cache in pages: new rows written, attended
+ *                           from, and the least attended slots given up
  *
  * Conventions shared by every call
  * --------------------------------
@@ -295,6 +299,104 @@ int d3tom_merge_kv(d3tom_ctx* ctx, d3tom_dtype dt, d3tom_agg mode,
                    void* k_out, void* v_out, const int32_t* cu_seqlens_out,
                    int32_t* assign, int32_t* member_count, int32_t* src_of_dst,
                    float* sim_debug, d3tom_stream stream);
+
+/* ------------------------------------------------------------------ a K/V cache in pages
+ * Sec. 4.4 (Compatibility with KV-Cache) merges a cached [visual | prompt] prefix; the calls below are what such a
+ * cache is filled, read and shortened with while the response is decoded.  The paper leaves this part to the host
+ * model; positions, pages and eviction follow the formulas given here.
+ *
+ * Slot j of request b is row j % page_size of page page_table[b][j / page_size].  A request has length[b] slots, in no
+ * order that attention depends on: keys are stored with their positions already in them. */
+typedef struct {
+  void* k;                      /* [pages, page_size, kv_heads, dh] storage type */
+  void* v;                      /* [pages, page_size, kv_heads, dh] storage type */
+  float* weight;                /* [pages, page_size] attention mass a slot has drawn; may be NULL where no call needs it */
+  int32_t* token;               /* [pages, page_size] the number its owner gave a slot's token; may be NULL likewise */
+  const int32_t* page_table;    /* [B, max_pages] pages of each request; entries behind its last page are not looked at */
+  const int32_t* length;        /* [B] slots of each request */
+  int pages, page_size;
+  int kv_heads;                 /* divides the context's heads: query head h reads key head h / (heads / kv_heads) */
+  int max_pages;
+} d3tom_cache;
+
+typedef enum { D3TOM_PAIR_HALVES = 0, D3TOM_PAIR_NEIGHBOURS = 1 } d3tom_pairing;
+typedef enum { D3TOM_LADDER_SHARED = 0, D3TOM_LADDER_PER_AXIS = 1 } d3tom_ladder;
+typedef enum { D3TOM_WEIGHT_NONE = 0, D3TOM_WEIGHT_ADD = 1, D3TOM_WEIGHT_SET = 2 } d3tom_weight_mode;
+
+/* Rotary positions: n = section[0] + .. + section[axes - 1] pairs of every head's dh numbers are rotated, the numbers
+ * from 2 n on are copied.  Pair i is (x[i], x[n + i]) with D3TOM_PAIR_HALVES, (x[2 i], x[2 i + 1]) with
+ * D3TOM_PAIR_NEIGHBOURS.  The first section[0] pairs turn with a row's position on axis 0 (time), the next section[1]
+ * on axis 1 (height), then axis 2 (width), by position * theta^-e radians, e = i / n with D3TOM_LADDER_SHARED and
+ * (i - first pair of the axis) / section[axis] with D3TOM_LADDER_PER_AXIS. */
+typedef struct {
+  double theta;                 /* >= 1 */
+  int axes;                     /* 1, 2 or 3 */
+  int section[3];               /* pairs of each axis, >= 0; their sum is between 1 and dh / 2 */
+  int pairing;                  /* d3tom_pairing */
+  int ladder;                   /* d3tom_ladder */
+} d3tom_rope_spec;
+
+/* q_out, k_out = the rows of q and k rotated by their positions; inverse != 0 rotates back (the same call takes the
+ * gradient of a rotation's output to its input).  q [rows, H, dh], k [rows, kv_heads, dh] or NULL (with k_out NULL);
+ * positions [rows, axes] int32, any value.  q_out may be q and k_out may be k; otherwise the buffers must not overlap.
+ * Angles are exact to 2^-32 of a turn at every position; cosine and sine are rounded to fp32, the result once to the
+ * storage type.  All row buffers must be 16-byte aligned. */
+int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
+               const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
+               d3tom_stream stream);
+
+/* Writes new rows into the LAST slots of their requests: row i of the n = cu_rows[b+1] - cu_rows[b] new rows of request
+ * b goes to slot length[b] - n + i, so length counts the new rows already (the caller advances it first).
+ *  spec       rotary positions of q and k; NULL: none (keys that have theirs, or a model without)
+ *  q          [total_rows, H, dh] or NULL; q_out [total_rows, H, dh] gets it rotated (may be q)
+ *  k, v       [total_rows, kv_heads, dh]
+ *  positions  [total_rows, axes] int32 (NULL without spec)
+ *  tokens     [total_rows] int32 numbers for cache->token (NULL: cache->token is left alone)
+ *  first_weight  [total_rows] fp32 for cache->weight (NULL: 0); +inf keeps a slot from being evicted
+ *  cu_rows    [B+1] int32, prefix sum of the new rows; total_rows == cu_rows[B] (host copy); rows behind cu_rows[B]
+ *             are neither read nor written
+ * Two rows of one call must not have the same slot.  A row whose slot does not exist is dropped (see d3tom_attn_cached).
+ * Row buffers, cache->k and cache->v must be 16-byte aligned. */
+int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const d3tom_rope_spec* spec,
+                       const void* q, const void* k, const void* v, const int32_t* positions, const int32_t* tokens,
+                       const float* first_weight, const int32_t* cu_rows, int B, int total_rows, void* q_out,
+                       d3tom_stream stream);
+
+/* Attention of new rows (one token, or a response block) over everything their request has cached, no mask:
+ *   out_i,h = sum_j A_ihj v_j,  A_ih = softmax_j(q_i,h . k_j * softmax_scale),  j over the length[b] slots.
+ * With mode D3TOM_WEIGHT_ADD / D3TOM_WEIGHT_SET the attention mass of every slot,
+ *   mass_j = sum_i row_weight_i sum_h A_ihj,
+ * is added to / stored in cache->weight (the importance of Sec. 3.2.1, S_j, when the rows are the deciders, or
+ * row_weight is 1 for deciders and 0 for the others).  Sums run in a fixed order: results are run-to-run identical.
+ *  q           [total_rows, H, dh]; rows [cu_rows[b], cu_rows[b+1]) belong to request b; rows behind cu_rows[B] are
+ *              neither read nor written
+ *  max_rows    host: >= every request's rows;  max_length  host: >= every length[b] (smaller values cost time or cut)
+ *  row_weight  [total_rows] fp32 or NULL (all 1)
+ *  out         [total_rows, H*dh]; rows of a request without slots are zero
+ * The weights need scratch of the context's decider scores: total_rows <= max_deciders and max_length <=
+ * max_visual_per_request, D3TOM_ERR_WORKSPACE otherwise.  bf16 on the tensor-core path needs page_size % 8 == 0
+ * (D3TOM_ERR_UNSUPPORTED otherwise).  q, out, cache->k and cache->v must be 16-byte aligned.
+ * What the device finds wrong: a slot behind max_length or behind the table, or on a page outside [0, pages), does not
+ * exist for this call and the other two (it is not read, written or moved), a negative length is 0, and the status word
+ * (d3tom_device_status) says D3TOM_ERR_INVALID_ARG. */
+int d3tom_attn_cached(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const void* q, const int32_t* cu_rows,
+                      int B, int total_rows, int max_rows, int max_length, float softmax_scale, d3tom_weight_mode mode,
+                      const float* row_weight, void* out, d3tom_stream stream);
+
+/* Every request gives up its lightest slots: of its length[b] slots the min(budget[b], length[b]) first ones by
+ * (weight descending, slot ascending) stay; slots whose token number is >= protect_from[b], and slots whose weight is
+ * not a number, come before all others (among themselves by slot).  The new length n is stored in length_out[b]; the
+ * i-th kept slot at or behind n moves (k, v, weight, token) into the i-th given-up slot before n.  Nothing else moves:
+ * slots kept below n stay where they are, slots behind n are left as they were, and pages behind the new last one are
+ * the caller's again.
+ *  budget        [B] int32 (negative counts as 0)
+ *  protect_from  [B] int32 or NULL (no slot is protected); needs cache->token
+ *  length_out    [B] int32; may be the array cache->length
+ *  max_length    host: >= every length[b]
+ * No two requests of a call may share a page that is moved into.  Scratch: B * (max_length + 3) words out of
+ * max_total_tokens * heads * dh, D3TOM_ERR_WORKSPACE beyond. */
+int d3tom_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const int32_t* budget,
+                      const int32_t* protect_from, int B, int max_length, int32_t* length_out, d3tom_stream stream);
 
 /* Sec. 3.2.2, last paragraph: the layers after l* run on the shortened tensor.
  * Same attention as d3tom_attn_importance, over packed ragged sequences, with

@@ -19,6 +19,9 @@ LIB_PATH = os.path.join(_HERE, "libd3tom.so")
 
 BF16, FP32 = 0, 1
 AGG_SUM, AGG_MEAN = 0, 1
+PAIR_HALVES, PAIR_NEIGHBOURS = 0, 1
+LADDER_SHARED, LADDER_PER_AXIS = 0, 1
+WEIGHT_NONE, WEIGHT_ADD, WEIGHT_SET = 0, 1, 2
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = -1, -2, -3, -4, -5
 
@@ -26,6 +29,46 @@ ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = -1, -2,
 class Limits(C.Structure):
     _fields_ = [("max_total_tokens", C.c_int), ("max_batch", C.c_int), ("heads", C.c_int), ("head_dim", C.c_int),
                 ("max_deciders", C.c_int), ("max_visual_per_request", C.c_int)]
+
+
+class RopeSpec(C.Structure):
+    """Rotary positions: pairs per axis (time, height, width), base, how pairs and frequencies are laid out
+    (d3tom_rope_spec)."""
+    _fields_ = [("theta", C.c_double), ("axes", C.c_int), ("section", C.c_int * 3), ("pairing", C.c_int),
+                ("ladder", C.c_int)]
+
+    def __init__(self, section, theta: float = 10000.0, pairing: int = PAIR_HALVES, ladder: int = LADDER_SHARED):
+        section = [int(x) for x in section]
+        if not 1 <= len(section) <= 3:
+            raise ValueError("one to three axes")
+        super().__init__(theta, len(section), (C.c_int * 3)(*section), pairing, ladder)
+
+
+class _CacheStruct(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("weight", C.c_void_p), ("token", C.c_void_p),
+                ("page_table", C.c_void_p), ("length", C.c_void_p), ("pages", C.c_int), ("page_size", C.c_int),
+                ("kv_heads", C.c_int), ("max_pages", C.c_int)]
+
+
+class Cache:
+    """A K/V cache in pages (d3tom_cache): k, v [pages, page_size, kv_heads, dh]; weight fp32 and token int32
+    [pages, page_size], either None where no call needs it; page_table [B, max_pages] and length [B] int32.  Holds the
+    tensors; their contents may change between calls."""
+
+    def __init__(self, k, v, weight, token, page_table, length):
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v are [pages, page_size, kv_heads, head_dim] of one type")
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or length.dtype != torch.int32 \
+                or length.numel() < page_table.shape[0]:
+            raise ValueError("page_table is [B, max_pages] int32, length [B] int32")
+        for t, dt in ((weight, torch.float32), (token, torch.int32)):
+            if t is not None and (t.shape != k.shape[:2] or t.dtype != dt):
+                raise ValueError("weight (fp32) and token (int32) are [pages, page_size]")
+        self.tensors = (k, v, weight, token, page_table, length)
+        self.k, self.v, self.weight, self.token, self.page_table, self.length = self.tensors
+        self.dt = _dt(k)
+        self._struct = _CacheStruct(*(_ptr(t) for t in self.tensors), k.shape[0], k.shape[1], k.shape[2], page_table.shape[1])
+        self.ref = C.byref(self._struct)
 
 
 class D3tomError(RuntimeError):
@@ -60,6 +103,10 @@ _SIGNATURES = {
     "d3tom_select": (_I, [_P, _P, _P, _P, _P, _I, _I, _P, _P, _P]),
     "d3tom_merge": (_I, [_P, _I, _I, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P]),
     "d3tom_merge_kv": (_I, [_P, _I, _I, _P, _P, _P, _P, _P, _P, _P, _I, _I, _I, _I, _I, _I, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "d3tom_rope": (_I, [_P, _I, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P]),
+    "d3tom_cache_append": (_I, [_P, _I, _P, _P, _P, _P, _P, _P, _P, _P, _P, _I, _I, _P, _P]),
+    "d3tom_attn_cached": (_I, [_P, _I, _P, _P, _P, _I, _I, _I, _I, _F, _I, _P, _P, _P]),
+    "d3tom_cache_evict": (_I, [_P, _I, _P, _P, _P, _I, _I, _P, _P]),
     "d3tom_attn_varlen": (_I, [_P, _I, _P, _P, _P, _P, _I, _I, _I, _F, _P, _P]),
     "d3tom_proj_qkv": (_I, [_P, _I, _P, _P, _I, _I, _P, _P, _P, _P]),
     "d3tom_linear": (_I, [_P, _I, _P, _P, _P, _I, _I, _I, _P, _P]),
@@ -257,3 +304,28 @@ class Context:
         _check(load().d3tom_ffn(self._h, _dt(x), _ptr(x), _ptr(w_gate_up), _ptr(w_down),
                                 _ptr(residual) if residual is not None else None, rows, D, m, _ptr(act), _ptr(out),
                                 _stream(stream)), "d3tom_ffn")
+
+    # -------------------------------------------------------------- a K/V cache in pages
+    def d3tom_rope(self, spec, q, k, positions, rows, kv_heads, q_out, k_out, inverse=False, stream=None):
+        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _ptr(q), _ptr(k), _ptr(positions), rows, kv_heads,
+                                 int(inverse), _ptr(q_out), _ptr(k_out), _stream(stream)), "d3tom_rope")
+
+    def d3tom_cache_append(self, cache, spec, q, k, v, positions, tokens, first_weight, cu_rows, B, total_rows, q_out,
+                           stream=None):
+        if cache.dt != _dt(k) or (q is not None and cache.dt != _dt(q)):
+            raise TypeError("rows and cache are of one storage type")
+        _check(load().d3tom_cache_append(self._h, cache.dt, cache.ref, None if spec is None else C.byref(spec), _ptr(q), _ptr(k),
+                                         _ptr(v), _ptr(positions), _ptr(tokens), _ptr(first_weight), _ptr(cu_rows), B,
+                                         total_rows, _ptr(q_out), _stream(stream)), "d3tom_cache_append")
+
+    def d3tom_attn_cached(self, cache, q, cu_rows, B, total_rows, max_rows, max_length, softmax_scale, mode, row_weight, out,
+                          stream=None):
+        if cache.dt != _dt(q) or cache.dt != _dt(out):
+            raise TypeError("rows and cache are of one storage type")
+        _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _ptr(q), _ptr(cu_rows), B, total_rows, max_rows,
+                                        max_length, softmax_scale, mode, _ptr(row_weight), _ptr(out), _stream(stream)),
+               "d3tom_attn_cached")
+
+    def d3tom_cache_evict(self, cache, budget, protect_from, B, max_length, length_out, stream=None):
+        _check(load().d3tom_cache_evict(self._h, cache.dt, cache.ref, _ptr(budget), _ptr(protect_from), B, max_length,
+                                        _ptr(length_out), _stream(stream)), "d3tom_cache_evict")

@@ -60,6 +60,8 @@ void free_all(d3tom_ctx* c) {
 
 bool dtype_ok(d3tom_dtype dt) { return dt == D3TOM_BF16 || dt == D3TOM_FP32; }
 
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
 // bf16 on tensor cores needs dh in {64, 128}; the CUDA-core kernels take dh % 4 == 0, dh <= 128
 int check_head_dim(const d3tom_ctx* ctx, d3tom_dtype dt) {
   const int dh = ctx->lim.head_dim;
@@ -442,6 +444,184 @@ int d3tom_ffn(d3tom_ctx* ctx, d3tom_dtype dt, const void* x, const void* w_gate_
   const int st = launch_gate_up_simt(ctx, dt, x, w_gate_up, rows, D, m, act, s);
   if (st != D3TOM_OK) return st;
   return launch_linear_simt(ctx, dt, act, w_down, residual, rows, m, D, out, s);
+}
+
+// ------------------------------------------------------------------ a K/V cache in pages
+
+// The turns of every pair per position step, and its axis, from a rotary description.
+static int make_rope_table(const d3tom_rope_spec* sp, int dh, RopeTable* t) {
+  if (sp->axes < 1 || sp->axes > 3 || !(sp->theta >= 1.0) || !isfinite(sp->theta)) return D3TOM_ERR_INVALID_ARG;
+  if ((sp->pairing != D3TOM_PAIR_HALVES && sp->pairing != D3TOM_PAIR_NEIGHBOURS) ||
+      (sp->ladder != D3TOM_LADDER_SHARED && sp->ladder != D3TOM_LADDER_PER_AXIS))
+    return D3TOM_ERR_INVALID_ARG;
+  int n = 0;
+  for (int a = 0; a < sp->axes; ++a) {
+    if (sp->section[a] < 0 || sp->section[a] > dh / 2 - n) return D3TOM_ERR_INVALID_ARG;
+    n += sp->section[a];
+  }
+  if (n < 1 || n > 64) return D3TOM_ERR_INVALID_ARG;
+  t->pairs = n; t->axes = sp->axes; t->neighbours = sp->pairing == D3TOM_PAIR_NEIGHBOURS;
+  for (int a = 0, first = 0; a < sp->axes; first += sp->section[a], ++a)
+    for (int i = first; i < first + sp->section[a]; ++i) {
+      const double e = sp->ladder == D3TOM_LADDER_PER_AXIS ? (double)(i - first) / sp->section[a] : (double)i / n;
+      // theta^-e <= 1 radian, a part of a turn below 1/6: as a 64-bit fraction the product with any position wraps
+      // around at whole turns, which is what an angle does
+      t->turn[i] = (unsigned long long)(pow(sp->theta, -e) * (18446744073709551616.0 / 6.283185307179586476925));
+      t->axis[i] = (unsigned char)a;
+    }
+  return D3TOM_OK;
+}
+
+static int rope_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
+                     const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
+                     cudaStream_t s) {
+  if (ctx == nullptr || spec == nullptr || q == nullptr || q_out == nullptr || positions == nullptr ||
+      (k == nullptr) != (k_out == nullptr) || rows < 0 || (k != nullptr && kv_heads <= 0))
+    return D3TOM_ERR_INVALID_ARG;
+  if (!dtype_ok(dt)) return D3TOM_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out)) return D3TOM_ERR_INVALID_ARG;
+  const int dh = ctx->lim.head_dim;
+  if (dh % 4 != 0 || dh > 128 || (dt == D3TOM_BF16 && dh % 8 != 0)) return D3TOM_ERR_UNSUPPORTED;
+  if (rows > ctx->lim.max_total_tokens || kv_heads > ctx->lim.heads) return D3TOM_ERR_WORKSPACE;
+  RopeTable t = {};
+  const int st = make_rope_table(spec, dh, &t);
+  if (st != D3TOM_OK || rows == 0) return st;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return D3TOM_ERR_CUDA;
+  RotateArgs a = {};
+  a.q = q; a.k = k; a.q_out = q_out; a.k_out = k_out; a.positions = positions; a.rows = rows;
+  a.H = ctx->lim.heads; a.kv_heads = k != nullptr ? kv_heads : 0; a.dh = dh; a.inverse = inverse != 0;
+  a.dev_status = ctx->dev_status;
+  return launch_rotate(ctx, dt, a, t, false, s);
+}
+
+int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
+               const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
+               d3tom_stream stream) {
+  return logged(rope_impl(ctx, dt, spec, q, k, positions, rows, kv_heads, inverse, q_out, k_out, static_cast<cudaStream_t>(stream)),
+                "d3tom_rope dt %d rows %d kv_heads %d inverse %d", (int)dt, rows, kv_heads, inverse);
+}
+
+// What the calls on a cache have in common.
+static int check_cache(const d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c, int B) {
+  if (ctx == nullptr || c == nullptr || c->k == nullptr || c->v == nullptr || c->page_table == nullptr || c->length == nullptr)
+    return D3TOM_ERR_INVALID_ARG;
+  if (!dtype_ok(dt)) return D3TOM_ERR_UNSUPPORTED;
+  if (B <= 0 || c->pages <= 0 || c->page_size <= 0 || c->kv_heads <= 0 || c->max_pages < 0 || ctx->lim.heads % c->kv_heads != 0 ||
+      !aligned16(c->k) || !aligned16(c->v))
+    return D3TOM_ERR_INVALID_ARG;
+  if ((long long)c->pages * c->page_size > 0x7fffffffll - 128 || (long long)c->max_pages * c->page_size > 0x7fffffffll - 128)
+    return D3TOM_ERR_UNSUPPORTED;               // slots are counted in 32 bits
+  if (B > ctx->lim.max_batch) return D3TOM_ERR_WORKSPACE;
+  return D3TOM_OK;
+}
+
+static int append_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const d3tom_rope_spec* spec, const void* q,
+                       const void* k, const void* v, const int32_t* positions, const int32_t* tokens,
+                       const float* first_weight, const int32_t* cu_rows, int B, int total_rows, void* q_out,
+                       cudaStream_t s) {
+  int st = check_cache(ctx, dt, cache, B);
+  if (st != D3TOM_OK) return st;
+  if (k == nullptr || v == nullptr || cu_rows == nullptr || total_rows < 0 || (q == nullptr) != (q_out == nullptr) ||
+      (spec != nullptr && positions == nullptr) || (tokens != nullptr && cache->token == nullptr) ||
+      (first_weight != nullptr && cache->weight == nullptr))
+    return D3TOM_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return D3TOM_ERR_INVALID_ARG;
+  const int dh = ctx->lim.head_dim;
+  if (dh % 4 != 0 || dh > 128 || (dt == D3TOM_BF16 && dh % 8 != 0)) return D3TOM_ERR_UNSUPPORTED;
+  if (total_rows > ctx->lim.max_total_tokens) return D3TOM_ERR_WORKSPACE;
+  RopeTable t = {};
+  if (spec != nullptr) st = make_rope_table(spec, dh, &t);
+  if (st != D3TOM_OK || total_rows == 0) return st;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return D3TOM_ERR_CUDA;
+  RotateArgs a = {};
+  a.q = q; a.k = k; a.v = v; a.q_out = q_out; a.positions = positions; a.rows = total_rows;
+  a.H = q != nullptr ? ctx->lim.heads : 0; a.kv_heads = cache->kv_heads; a.dh = dh;
+  a.cache = *cache; a.tokens = tokens; a.first_weight = first_weight; a.cu_rows = cu_rows; a.B = B;
+  a.dev_status = ctx->dev_status;
+  return launch_rotate(ctx, dt, a, t, true, s);
+}
+
+int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const d3tom_rope_spec* spec,
+                       const void* q, const void* k, const void* v, const int32_t* positions, const int32_t* tokens,
+                       const float* first_weight, const int32_t* cu_rows, int B, int total_rows, void* q_out,
+                       d3tom_stream stream) {
+  return logged(append_impl(ctx, dt, cache, spec, q, k, v, positions, tokens, first_weight, cu_rows, B, total_rows, q_out,
+                            static_cast<cudaStream_t>(stream)),
+                "d3tom_cache_append dt %d B %d rows %d", (int)dt, B, total_rows);
+}
+
+static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const void* q, const int32_t* cu_rows,
+                            int B, int total_rows, int max_rows, int max_length, float softmax_scale,
+                            d3tom_weight_mode mode, const float* row_weight, void* out, cudaStream_t s) {
+  int st = check_cache(ctx, dt, cache, B);
+  if (st != D3TOM_OK) return st;
+  if (q == nullptr || out == nullptr || cu_rows == nullptr || total_rows < 0 || max_rows < 0 || max_rows > total_rows ||
+      max_length < 0 || !(softmax_scale > 0.f) || !isfinite(softmax_scale) || !aligned16(q) || !aligned16(out))
+    return D3TOM_ERR_INVALID_ARG;
+  if (mode != D3TOM_WEIGHT_NONE && mode != D3TOM_WEIGHT_ADD && mode != D3TOM_WEIGHT_SET) return D3TOM_ERR_INVALID_ARG;
+  if (mode != D3TOM_WEIGHT_NONE && cache->weight == nullptr) return D3TOM_ERR_INVALID_ARG;
+  if (total_rows > ctx->lim.max_total_tokens) return D3TOM_ERR_WORKSPACE;
+  if (mode != D3TOM_WEIGHT_NONE && (total_rows > ctx->lim.max_deciders || max_length > ctx->lim.max_visual_per_request))
+    return D3TOM_ERR_WORKSPACE;
+  st = check_head_dim(ctx, dt);
+  if (st != D3TOM_OK) return st;
+  const bool tensor = dt == D3TOM_BF16 && !ctx->reference_kernels;
+  if (tensor && cache->page_size % 8 != 0) return D3TOM_ERR_UNSUPPORTED;
+  if ((long long)total_rows * ctx->lim.heads > 0x7fffffffll) return D3TOM_ERR_UNSUPPORTED;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return D3TOM_ERR_CUDA;
+  CachedArgs a = {};
+  a.q = q; a.out = out; a.k = cache->k; a.v = cache->v; a.cu_rows = cu_rows;
+  a.page_table = cache->page_table; a.length = cache->length;
+  a.B = B; a.H = ctx->lim.heads; a.dh = ctx->lim.head_dim; a.kv_heads = cache->kv_heads; a.group = a.H / a.kv_heads;
+  a.total_rows = total_rows; a.max_rows = max_rows;
+  a.pages = cache->pages; a.page_size = cache->page_size; a.max_pages = cache->max_pages;
+  const long long slots = (long long)cache->max_pages * cache->page_size;
+  a.cap = max_length < slots ? max_length : (int)slots;
+  a.scale_log2 = softmax_scale * 1.4426950408889634f;
+  if (mode != D3TOM_WEIGHT_NONE) { a.scores = ctx->score_scratch; a.lse = ctx->lse_scratch; a.score_stride = ctx->vis_stride; }
+  a.part = ctx->attn_part_ws;
+  a.dev_status = ctx->dev_status;
+  if (total_rows > 0) {
+    st = launch_attn_cached_simt(ctx, dt, a, s);
+    if (st != D3TOM_OK) return st;
+  }
+  if (mode != D3TOM_WEIGHT_NONE && a.cap > 0)
+    st = launch_cached_weight(ctx, a, cache->weight, mode == D3TOM_WEIGHT_ADD, row_weight, a.cap, s);
+  return st;
+}
+
+int d3tom_attn_cached(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const void* q, const int32_t* cu_rows,
+                      int B, int total_rows, int max_rows, int max_length, float softmax_scale, d3tom_weight_mode mode,
+                      const float* row_weight, void* out, d3tom_stream stream) {
+  return logged(attn_cached_impl(ctx, dt, cache, q, cu_rows, B, total_rows, max_rows, max_length, softmax_scale, mode,
+                                 row_weight, out, static_cast<cudaStream_t>(stream)),
+                "d3tom_attn_cached dt %d B %d rows %d max_rows %d max_length %d weights %d", (int)dt, B, total_rows, max_rows,
+                max_length, (int)mode);
+}
+
+static int evict_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const int32_t* budget,
+                      const int32_t* protect_from, int B, int max_length, int32_t* length_out, cudaStream_t s) {
+  int st = check_cache(ctx, dt, cache, B);
+  if (st != D3TOM_OK) return st;
+  if (cache->weight == nullptr || budget == nullptr || length_out == nullptr || max_length < 0 ||
+      (protect_from != nullptr && cache->token == nullptr))
+    return D3TOM_ERR_INVALID_ARG;
+  const int row_bytes = ctx->lim.head_dim * (dt == D3TOM_BF16 ? 2 : 4);
+  if (row_bytes % 8 != 0) return D3TOM_ERR_UNSUPPORTED;
+  if ((long long)B * ((long long)max_length + 3) > (long long)ctx->lim.max_total_tokens * ctx->lim.heads * ctx->lim.head_dim)
+    return D3TOM_ERR_WORKSPACE;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return D3TOM_ERR_CUDA;
+  return launch_cache_evict(ctx, dt, *cache, budget, protect_from, B, max_length, length_out, s);
+}
+
+int d3tom_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const int32_t* budget,
+                      const int32_t* protect_from, int B, int max_length, int32_t* length_out, d3tom_stream stream) {
+  return logged(evict_impl(ctx, dt, cache, budget, protect_from, B, max_length, length_out, static_cast<cudaStream_t>(stream)),
+                "d3tom_cache_evict dt %d B %d max_length %d", (int)dt, B, max_length);
 }
 
 }  // extern "C"

@@ -1,0 +1,133 @@
+// Which CTA attends to which keys of a cache in pages, and how the kernels of d3tom_attn_cached find slots.
+//
+// A work item is (request, key head, up to `tile_rows` of the request's rows x query heads of that key head); its keys
+// come in tiles of 128 slots.  The tiles of all items, in order, are dealt to the CTAs in equal runs: CTA c of C has
+// tiles [c W / C, (c + 1) W / C) of W, so a batch of very uneven lengths and one very long request load the SMs alike.
+// A run covers any number of whole items and at most one item's end at its beginning and one item's beginning at its
+// end: two partial results per CTA, kept at part[c][0] (the run's first segment) and part[c][1] (its last).  What each
+// CTA does follows from the lengths alone, so results do not depend on timing, and lengths that change between replays
+// of a graph are followed without the host.
+#pragma once
+
+#include "common.cuh"
+
+constexpr int kKeyTile = 128;
+
+struct CachedRequest {
+  int len, n, lo;               // slots, new rows, first packed row
+};
+__device__ __forceinline__ CachedRequest cached_request(const CachedArgs& a, int b) {
+  CachedRequest r;
+  const int len = a.length[b];
+  const int lo = min(max(a.cu_rows[b], 0), a.total_rows), hi = min(max(a.cu_rows[b + 1], 0), a.total_rows);
+  r.len = min(max(len, 0), a.cap);
+  r.lo = lo;
+  r.n = max(hi - lo, 0);
+  return r;
+}
+__device__ __forceinline__ int cached_row_tiles(const CachedArgs& a, int n) {
+  return (int)(((long long)n * a.group + a.tile_rows - 1) / a.tile_rows);
+}
+__device__ __forceinline__ int cached_key_tiles(int len) { return (len + kKeyTile - 1) / kKeyTile; }
+__device__ __forceinline__ long long cached_work(const CachedArgs& a, const CachedRequest& r) {
+  return (long long)a.kv_heads * cached_row_tiles(a, r.n) * cached_key_tiles(r.len);
+}
+
+// A CTA's run, and the request it begins in.
+struct CachedRun {
+  long long w0, w1, base, total;   // tiles [w0, w1) of `total`; the first tile of request b
+  int b, ctas;                     // ctas that have work
+};
+__device__ __forceinline__ long long cached_run_begin(long long total, int ctas, int c) { return total * c / ctas; }
+
+// Whole warp; the same answer in all lanes.
+__device__ __forceinline__ CachedRun cached_run(const CachedArgs& a, int cta) {
+  const int lane = threadIdx.x & 31;
+  long long total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    const int b = b0 + lane;
+    total += b < a.B ? cached_work(a, cached_request(a, b)) : 0;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  CachedRun run;
+  run.total = total;
+  run.ctas = total < a.ctas ? (int)total : a.ctas;
+  run.b = 0; run.base = 0; run.w0 = run.w1 = total;
+  if (cta >= run.ctas) return run;
+  run.w0 = cached_run_begin(total, run.ctas, cta);
+  run.w1 = cached_run_begin(total, run.ctas, cta + 1);
+  long long before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    const int b = b0 + lane;
+    const long long mine = b < a.B ? cached_work(a, cached_request(a, b)) : 0;
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += t;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + incl > run.w0);
+    if (hit != 0u) {
+      const int src = __ffs(hit) - 1;
+      run.b = b0 + src;
+      run.base = before + __shfl_sync(0xffffffffu, incl - mine, src);
+      return run;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return run;
+}
+
+// The segments of a run, one after the other.
+struct CachedSegment {
+  int b, len, lo, rows;         // request, its slots, its first packed row, rows x query heads of the tile
+  int kv_head, row0;            // key head; the tile's first (row x query head)
+  int t0, t1;                   // key tiles
+  bool whole;                   // the item has no other segment
+  int slot;                     // of part[cta] otherwise
+};
+struct CachedWalk {
+  long long w, w_begin, w_end, base, work;
+  int b, tiles, row_tiles;
+  CachedRequest r;
+
+  __device__ __forceinline__ void enter(const CachedArgs& a) {
+    r = cached_request(a, b);
+    tiles = cached_key_tiles(r.len);
+    row_tiles = cached_row_tiles(a, r.n);
+    work = (long long)a.kv_heads * row_tiles * tiles;
+  }
+  __device__ __forceinline__ void start(const CachedArgs& a, const CachedRun& run) {
+    w = w_begin = run.w0; w_end = run.w1; base = run.base; b = run.b;
+    if (w < w_end) enter(a);
+  }
+  __device__ __forceinline__ bool next(const CachedArgs& a, CachedSegment& s) {
+    if (w >= w_end) return false;
+    while (w >= base + work) { base += work; ++b; enter(a); }
+    const long long rel = w - base;
+    const int item = (int)(rel / tiles);
+    s.t0 = (int)(rel - (long long)item * tiles);
+    s.t1 = (int)min((long long)tiles, s.t0 + (w_end - w));
+    s.whole = s.t0 == 0 && s.t1 == tiles;
+    s.slot = w == w_begin ? 0 : 1;
+    s.b = b; s.len = r.len; s.lo = r.lo;
+    s.kv_head = item / row_tiles;
+    s.row0 = (item - s.kv_head * row_tiles) * a.tile_rows;
+    s.rows = (int)min((long long)a.tile_rows, (long long)r.n * a.group - s.row0);
+    w += s.t1 - s.t0;
+    return true;
+  }
+};
+
+// The rank of row x query head f of a request among all [total_rows * H]: packed row * H + query head.
+__device__ __forceinline__ int cached_row_index(const CachedArgs& a, const CachedSegment& s, int r) {
+  const int f = s.row0 + r, i = f / a.group;
+  return (s.lo + i) * a.H + s.kv_head * a.group + (f - i * a.group);
+}
+
+// The slot's place in the pools, -1 where its page is not one of them.
+__device__ __forceinline__ long long cached_place(const int32_t* table, int slot, int page_size, int pages) {
+  const int p = slot / page_size, page = table[p];
+  return page < 0 || page >= pages ? -1 : (long long)page * page_size + (slot - p * page_size);
+}

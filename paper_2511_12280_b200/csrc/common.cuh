@@ -218,3 +218,36 @@ int launch_linear_simt(d3tom_ctx* ctx, d3tom_dtype dt, const void* x, const void
                        int K, int N, void* out, cudaStream_t s);
 int launch_gate_up_simt(d3tom_ctx* ctx, d3tom_dtype dt, const void* x, const void* w_gate_up, int rows, int D, int m,
                         void* act, cudaStream_t s);
+
+// A K/V cache in pages (d3tom_cache_append, d3tom_attn_cached, d3tom_cache_evict).
+struct RopeTable {
+  unsigned long long turn[64];  // per pair: turns a position step makes, in 2^-64 of a turn
+  unsigned char axis[64];
+  int pairs, axes, neighbours;
+};
+struct RotateArgs {
+  const void* q; const void* k; const void* v; void* q_out; void* k_out;
+  const int32_t* positions; int rows, H, kv_heads, dh, inverse;
+  // with a cache: where the rows go
+  d3tom_cache cache; const int32_t* tokens; const float* first_weight; const int32_t* cu_rows; int B;
+  int* dev_status;
+};
+int launch_rotate(d3tom_ctx* ctx, d3tom_dtype dt, const RotateArgs& a, const RopeTable& t, bool to_cache, cudaStream_t s);
+
+struct CachedArgs {
+  const void* q; void* out; const void* k; const void* v;
+  const int32_t* cu_rows; const int32_t* page_table; const int32_t* length;
+  int B, H, dh, kv_heads, group, total_rows, max_rows;
+  int pages, page_size, max_pages, cap;   // cap: slots a request can have in this call
+  float scale_log2;             // softmax_scale * log2(e)
+  float* scores; float2* lse; int score_stride;   // [total_rows][H][score_stride] raw q.k and [total_rows][H] (M, l); null without weights
+  float* part;                  // [ctas][2][tile_rows][dh + 2]: tiles of a work item that several CTAs share
+  int tile_rows, ctas;          // set by the launcher
+  int* dev_status;
+};
+int launch_attn_cached_simt(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
+int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
+int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, const float* row_weight,
+                         int max_length, cudaStream_t s);
+int launch_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache& cache, const int32_t* budget,
+                       const int32_t* protect_from, int B, int max_length, int32_t* length_out, cudaStream_t s);
