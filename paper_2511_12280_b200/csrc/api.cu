@@ -585,7 +585,7 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
   a.part = ctx->attn_part_ws;
   a.dev_status = ctx->dev_status;
   if (total_rows > 0) {
-    st = launch_attn_cached_simt(ctx, dt, a, s);
+    st = tensor ? launch_attn_cached_tc(ctx, a, s) : launch_attn_cached_simt(ctx, dt, a, s);
     if (st != D3TOM_OK) return st;
   }
   if (mode != D3TOM_WEIGHT_NONE && a.cap > 0)

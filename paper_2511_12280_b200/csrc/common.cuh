@@ -246,6 +246,7 @@ struct CachedArgs {
   int* dev_status;
 };
 int launch_attn_cached_simt(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
+int launch_attn_cached_tc(d3tom_ctx* ctx, const CachedArgs& a, cudaStream_t s);
 int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
 int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, const float* row_weight,
                          int max_length, cudaStream_t s);
