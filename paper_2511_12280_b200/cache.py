@@ -1,0 +1,88 @@
+"""A K/V cache in pages for one layer, from prefix to response block:
+
+    append (prefix, keys rotated)  ->  per step: append (block) -> attend -> evict or drop the block
+
+``PagedCache`` owns the pools, hands out pages and keeps the host's copy of the lengths (all sizes are known on the host, as
+everywhere in this package); every step of the path runs in the library's kernels.  Slots of a request are in no order that
+matters to attention; ``token`` holds the number that the caller gave a slot's token.
+"""
+from __future__ import annotations
+
+from typing import Optional, Sequence
+
+import numpy as np
+import torch
+
+from . import binding as B_
+
+
+class PagedCache:
+    def __init__(self, batch: int, heads: int, kv_heads: int, head_dim: int, dtype: torch.dtype, pages: int, page_size: int,
+                 max_rows: int, max_length: int, max_scored_rows: int = 1, device: int = 0):
+        """max_rows: new rows per call over the batch; max_length: slots of a request; max_scored_rows: rows of a call that
+        feeds the weights."""
+        self.dev = torch.device("cuda", device)
+        self.batch, self.heads, self.kv_heads, self.dh, self.dtype = batch, heads, kv_heads, head_dim, dtype
+        self.page_size, self.max_length = page_size, max_length
+        # the scratch of an eviction is counted in words of max_total_tokens rows
+        tokens = max(max_rows, -(-batch * (max_length + 3) // (heads * head_dim)))
+        self.ctx = B_.Context(tokens, batch, heads, head_dim, max(1, max_scored_rows), max(1, max_length), device)
+        shape = (pages, page_size)
+        kw = dict(device=self.dev)
+        self.k = torch.zeros(*shape, kv_heads, head_dim, dtype=dtype, **kw)
+        self.v = torch.zeros_like(self.k)
+        self.weight = torch.zeros(shape, dtype=torch.float32, **kw)
+        self.token = torch.zeros(shape, dtype=torch.int32, **kw)
+        self.table_h = np.full((batch, -(-max_length // page_size)), -1, dtype=np.int32)
+        self.table = torch.as_tensor(self.table_h, device=self.dev)
+        self.length = torch.zeros(batch, dtype=torch.int32, **kw)
+        self.cache = B_.Cache(self.k, self.v, self.weight, self.token, self.table, self.length)
+        self.lengths_h = [0] * batch
+        self.free = list(range(pages - 1, -1, -1))
+        self.scale = 1.0 / float(np.sqrt(head_dim))
+
+    def _resize(self, lengths: Sequence[int]):
+        """Pages for the new lengths; table and lengths on the device follow in stream order."""
+        need = [-(-n // self.page_size) for n in lengths]
+        have = [-(-n // self.page_size) for n in self.lengths_h]
+        if max(lengths) > self.max_length or sum(max(0, n - h) for n, h in zip(need, have)) > len(self.free):
+            raise RuntimeError("the cache is full: %s slots asked for" % (list(lengths),))
+        for b, (n, h) in enumerate(zip(need, have)):
+            for p in range(n, h):
+                self.free.append(int(self.table_h[b, p]))
+                self.table_h[b, p] = -1
+        for b, (n, h) in enumerate(zip(need, have)):
+            for p in range(h, n):
+                self.table_h[b, p] = self.free.pop()
+        if need != have:
+            self.table.copy_(torch.from_numpy(self.table_h.copy()))
+        self.length.copy_(torch.tensor(list(lengths), dtype=torch.int32))
+        self.lengths_h = [int(n) for n in lengths]
+
+    def _cu(self, rows: Sequence[int]):
+        return torch.as_tensor(np.concatenate([[0], np.cumsum(rows)]).astype(np.int32), device=self.dev)
+
+    def append(self, rows: Sequence[int], k, v, tokens, q=None, q_out=None, spec: Optional[B_.RopeSpec] = None,
+               positions=None, first_weight=None, stream=None):
+        """Writes rows[b] new rows of every request behind its slots; q rotated alike goes to q_out.  first_weight +inf
+        keeps a row from being evicted."""
+        if len(rows) != self.batch:
+            raise ValueError("rows of every request")
+        self._resize([n + r for n, r in zip(self.lengths_h, rows)])
+        self.ctx.d3tom_cache_append(self.cache, spec, q, k, v, positions, tokens, first_weight, self._cu(rows), self.batch,
+                                    int(sum(rows)), q_out, stream)
+
+    def attend(self, rows: Sequence[int], q, out, mode: int = B_.WEIGHT_NONE, row_weight=None, stream=None):
+        """Attention of rows[b] rows of every request over all of its slots."""
+        self.ctx.d3tom_attn_cached(self.cache, q, self._cu(rows), self.batch, int(sum(rows)), max(rows), max(self.lengths_h),
+                                   self.scale, mode, row_weight, out, stream)
+
+    def evict(self, budget: Sequence[int], protect_from=None, stream=None):
+        """Keeps the min(budget[b], length) heaviest slots of every request; frees the pages behind them."""
+        want = torch.as_tensor(np.asarray(budget, dtype=np.int32), device=self.dev)
+        self.ctx.d3tom_cache_evict(self.cache, want, protect_from, self.batch, max(self.lengths_h), self.length, stream)
+        self._resize([min(max(int(x), 0), n) for x, n in zip(budget, self.lengths_h)])
+
+    def drop_last(self, rows: Sequence[int]):
+        """Gives up the last rows[b] slots of every request (a block that the next step writes again)."""
+        self._resize([n - r for n, r in zip(self.lengths_h, rows)])
