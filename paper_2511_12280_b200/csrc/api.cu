@@ -55,7 +55,7 @@ void free_all(d3tom_ctx* c) {
   cudaFree(c->inv_norm_kept); cudaFree(c->kept_rows); cudaFree(c->best); cudaFree(c->member_off);
   cudaFree(c->member_cursor); cudaFree(c->member_list); cudaFree(c->heavy_slots); cudaFree(c->n_heavy); cudaFree(c->row_desc); cudaFree(c->agg_counter);
   cudaFree(c->gemm_split_ws); cudaFree(c->gemm_split_counters); cudaFree(c->dev_status);
-  cudaFree(c->attn_part_ws); cudaFree(c->attn_part_flags);
+  cudaFree(c->attn_part_ws); cudaFree(c->attn_part_flags); cudaFree(c->cached_joins);
 }
 
 bool dtype_ok(d3tom_dtype dt) { return dt == D3TOM_BF16 || dt == D3TOM_FP32; }
@@ -129,6 +129,7 @@ static int create_impl(d3tom_ctx** out, int device, const d3tom_limits* lim) {
   if (st == D3TOM_OK) st = alloc(c, &c->attn_part_ws, (size_t)c->sm_count * 2 * (128 + 2) * 128);
   if (st == D3TOM_OK) st = alloc(c, &c->attn_part_flags, (size_t)c->sm_count * 8);
   if (st == D3TOM_OK && cudaMemset(c->attn_part_flags, 0, (size_t)c->sm_count * 8 * sizeof(int)) != cudaSuccess) st = D3TOM_ERR_CUDA;
+  if (st == D3TOM_OK) st = alloc(c, &c->cached_joins, (size_t)3 * c->sm_count * 8);
   if (st == D3TOM_OK) st = alloc(c, &c->dev_status, 1);
   if (st == D3TOM_OK && cudaMemset(c->dev_status, 0, sizeof(int)) != cudaSuccess) st = D3TOM_ERR_CUDA;
   if (st != D3TOM_OK) { free_all(c); delete c; return st; }
@@ -582,7 +583,7 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
   a.cap = max_length < slots ? max_length : (int)slots;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   if (mode != D3TOM_WEIGHT_NONE) { a.scores = ctx->score_scratch; a.lse = ctx->lse_scratch; a.score_stride = ctx->vis_stride; }
-  a.part = ctx->attn_part_ws;
+  a.part = ctx->attn_part_ws; a.joins = ctx->cached_joins;
   a.dev_status = ctx->dev_status;
   if (total_rows > 0) {
     st = tensor ? launch_attn_cached_tc(ctx, a, s) : launch_attn_cached_simt(ctx, dt, a, s);

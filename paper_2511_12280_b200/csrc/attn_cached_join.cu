@@ -9,62 +9,63 @@
 
 namespace {
 
-constexpr int kJoinThreads = 128;
+constexpr int kJoinWarps = 4;
 
-// Block (c, y): if CTA c's run begins inside an item and contains its end, joins rows y, y + gridDim.y, .. of it.
-// The blocks also write what no CTA has: zeros for the rows of requests without slots.
+// Block (c, y), a warp per row: rows y * 4 .. + 3 of the item that ends in CTA c's run, where an earlier CTA began it.
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const CachedArgs a) {
+__global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const CachedArgs a) {
   grid_dependency_enter();
-  const int c = blockIdx.x, tid = threadIdx.x, dh = a.dh;
-  for (int b = c; b < a.B; b += gridDim.x) {
-    const CachedRequest r = cached_request(a, b);
-    const int raw = a.length[b];
-    if (tid == 0 && blockIdx.y == 0 && (raw < 0 || raw > a.cap)) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
-    if (r.len > 0) continue;
-    T* out = static_cast<T*>(a.out) + (size_t)r.lo * a.H * dh;
-    const size_t count = (size_t)r.n * a.H * dh;
-    for (size_t i = (size_t)blockIdx.y * kJoinThreads + tid; i < count; i += (size_t)gridDim.y * kJoinThreads)
-      out[i] = Storage<T>::from_float(0.f);
-  }
-  const CachedRun run = cached_run(a, c);
-  if (run.w0 >= run.w1) return;
-  CachedWalk walk;
-  walk.start(a, run);
-  CachedSegment s;
-  if (!walk.next(a, s) || s.t0 == 0 || s.t1 != walk.tiles) return;      // the run does not begin inside an item, or does not end it
-  const long long begin = run.w0 - s.t0;                                 // the item's first tile
-  int c0 = (int)(begin * run.ctas / run.total);                          // .. and the CTA that has it
-  while (cached_run_begin(run.total, run.ctas, c0) > begin) --c0;
-  while (cached_run_begin(run.total, run.ctas, c0 + 1) <= begin) ++c0;
-  const size_t stride = (size_t)a.tile_rows * (dh + 2);
-  const float* first = a.part + ((size_t)c0 * 2 + (cached_run_begin(run.total, run.ctas, c0) == begin ? 0 : 1)) * stride;
-  const float* rest = a.part + (size_t)(c0 + 1) * 2 * stride;
-  const int n = c - c0 + 1;
-  for (int r = blockIdx.y; r < s.rows; r += gridDim.y) {
-    // (O rows, then M of all rows, then l of all rows)
-    const size_t at_m = (size_t)a.tile_rows * dh + r, at_l = at_m + a.tile_rows;
-    float m = first[at_m];
-    for (int i = 1; i < n; ++i) m = fmaxf(m, rest[(size_t)(i - 1) * 2 * stride + at_m]);
-    float l = 0.f, o = 0.f;
-    for (int i = 0; i < n; ++i) {
-      const float* p = i == 0 ? first : rest + (size_t)(i - 1) * 2 * stride;
-      const float f = ptx::ex2(p[at_m] - m);
+  const int4 j0 = reinterpret_cast<const int4*>(a.joins)[2 * blockIdx.x];
+  const int n = j0.y, r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31, d = lane * 4, dh = a.dh;
+  if (r >= (n > 0 ? j0.w : 0)) return;
+  const int4 j1 = reinterpret_cast<const int4*>(a.joins)[2 * blockIdx.x + 1];
+  const size_t stride = cached_part_stride(a);
+  // part i: the first at `first`, the others at slot 0 of the CTAs after it
+  const size_t first = (size_t)j0.x, rest = (size_t)(j0.x / 2) * 2;
+  auto part = [&](int i) { return a.part + (i == 0 ? first : rest + 2 * (size_t)i) * stride; };
+  const size_t at_m = (size_t)a.tile_rows * dh + r, at_l = at_m + a.tile_rows;
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, part(i)[at_m]);
+  m = warp_max(m);
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = 0; i0 < n; i0 += 32) {
+    const int i = i0 + lane;
+    float f = 0.f;
+    if (i < n) {
+      const float* p = part(i);
+      f = ptx::ex2(p[at_m] - m);
       l += p[at_l] * f;
-      if (tid < dh) o += p[(size_t)r * dh + tid] * f;
     }
-    const int row = cached_row_index(a, s, r);
-    if (tid < dh) static_cast<T*>(a.out)[(size_t)row * dh + tid] = Storage<T>::from_float(l == 0.f ? 0.f : o / l);
-    if (tid == 0 && a.lse != nullptr) a.lse[row] = make_float2(m, l);
+    const int many = min(32, n - i0);
+#pragma unroll 8
+    for (int k = 0; k < many; ++k) {
+      const float g = __shfl_sync(0xffffffffu, f, k);
+      if (d < dh) {
+        const float4 x = *reinterpret_cast<const float4*>(part(i0 + k) + (size_t)r * dh + d);
+        o.x += x.x * g; o.y += x.y * g; o.z += x.z * g; o.w += x.w * g;
+      }
+    }
   }
+  l = warp_sum(l);
+  const int f = j1.y + r, i = f / a.group, row = (j0.z + i) * a.H + j1.x * a.group + (f - i * a.group);
+  if (d < dh) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* out = static_cast<T*>(a.out) + (size_t)row * dh + d;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    else *reinterpret_cast<uint2*>(out) = make_uint2(ptx::pack_bf16x2(o.x * inv, o.y * inv), ptx::pack_bf16x2(o.z * inv, o.w * inv));
+  }
+  if (lane == 0 && a.lse != nullptr) a.lse[row] = make_float2(m, l);
 }
 
-constexpr int kWeightWarps = 8;
+constexpr int kWeightRows = 1024;      // rows x heads whose (M, f / l) are in shared memory at a time
 
-// Block (b, x): 128 slots of request b, four per lane; the warps take every eighth row x head.
+// Block (b, x): 128 slots of request b, four per lane; the warps share its rows x heads.
+template <int kWeightWarps>
 __global__ void __launch_bounds__(kWeightWarps * 32)
 weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, const float* __restrict__ row_weight,
               const int chunks) {
+  __shared__ float2 ml[kWeightRows];
   __shared__ float4 sum[kWeightWarps][32];
   grid_dependency_enter();
   const int b = blockIdx.x / chunks, first = (blockIdx.x - b * chunks) * 128;
@@ -74,17 +75,27 @@ weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, con
   if (first >= r.len) return;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   const int rows = r.n * a.H;
-  if (slot0 < r.len) {                          // (the stride is a multiple of four: a float4 ends inside it)
-    const float* sc = a.scores + (size_t)r.lo * a.H * a.score_stride + slot0;
-    const float2* lse = a.lse + (size_t)r.lo * a.H;
-    for (int i = warp; i < rows; i += kWeightWarps) {
-      const float2 ml = lse[i];
-      const float4 s = *reinterpret_cast<const float4*>(sc + (size_t)i * a.score_stride);
-      const float f = ml.y == 0.f ? 0.f : (row_weight != nullptr ? row_weight[r.lo + i / a.H] : 1.f) / ml.y;
-      acc.x += f * ptx::ex2(fmaf(s.x, a.scale_log2, -ml.x));
-      acc.y += f * ptx::ex2(fmaf(s.y, a.scale_log2, -ml.x));
-      acc.z += f * ptx::ex2(fmaf(s.z, a.scale_log2, -ml.x));
-      acc.w += f * ptx::ex2(fmaf(s.w, a.scale_log2, -ml.x));
+  const bool has = slot0 < r.len;               // (the stride is a multiple of four: a float4 ends inside it)
+  for (int i0 = 0; i0 < rows; i0 += kWeightRows) {
+    const int many = min(kWeightRows, rows - i0);
+    if (i0 > 0) __syncthreads();
+    for (int i = threadIdx.x; i < many; i += kWeightWarps * 32) {
+      const float2 x = a.lse[(size_t)r.lo * a.H + i0 + i];
+      const float f = row_weight != nullptr ? row_weight[r.lo + (i0 + i) / a.H] : 1.f;
+      ml[i] = make_float2(-x.x, x.y == 0.f ? 0.f : f / x.y);
+    }
+    __syncthreads();
+    if (has) {
+      const float* sc = a.scores + ((size_t)r.lo * a.H + i0) * a.score_stride + slot0;
+#pragma unroll 8
+      for (int i = warp; i < many; i += kWeightWarps) {
+        const float2 f = ml[i];
+        const float4 s = __ldcs(reinterpret_cast<const float4*>(sc + (size_t)i * a.score_stride));
+        acc.x += f.y * ptx::ex2(fmaf(s.x, a.scale_log2, f.x));
+        acc.y += f.y * ptx::ex2(fmaf(s.y, a.scale_log2, f.x));
+        acc.z += f.y * ptx::ex2(fmaf(s.z, a.scale_log2, f.x));
+        acc.w += f.y * ptx::ex2(fmaf(s.w, a.scale_log2, f.x));
+      }
     }
   }
   sum[warp][lane] = acc;
@@ -104,9 +115,9 @@ weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, con
 }  // namespace
 
 int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s) {
-  const dim3 grid(a.ctas, a.tile_rows < 8 ? a.tile_rows : 8);
-  if (dt == D3TOM_BF16) D3TOM_CUDA_TRY(ctx, launch_serialized(join_kernel<__nv_bfloat16>, grid, kJoinThreads, 0, s, a));
-  else D3TOM_CUDA_TRY(ctx, launch_serialized(join_kernel<float>, grid, kJoinThreads, 0, s, a));
+  const dim3 grid(a.ctas, ceil_div(a.tile_rows, kJoinWarps));
+  if (dt == D3TOM_BF16) D3TOM_CUDA_TRY(ctx, launch_serialized(join_kernel<__nv_bfloat16>, grid, kJoinWarps * 32, 0, s, a));
+  else D3TOM_CUDA_TRY(ctx, launch_serialized(join_kernel<float>, grid, kJoinWarps * 32, 0, s, a));
   D3TOM_LAUNCH_CHECK(ctx);
   return D3TOM_OK;
 }
@@ -115,7 +126,10 @@ int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int
                          int max_length, cudaStream_t s) {
   const int chunks = ceil_div(max_length, 128);
   if ((long long)chunks * a.B > 0x7fffffffll) return D3TOM_ERR_UNSUPPORTED;
-  D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel, chunks * a.B, kWeightWarps * 32, 0, s, a, weight, add, row_weight, chunks));
+  // few rows: small blocks, many of them on an SM (64 requests of one row x 32 heads: 14 us with 8 warps, 30 with 16); many
+  // rows: the loads of a block side by side (32 rows x 32 heads: 80 us with 8 warps one after the other, 21 with 16)
+  if ((long long)a.max_rows * a.H <= 256) D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<4>, chunks * a.B, 4 * 32, 0, s, a, weight, add, row_weight, chunks));
+  else D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<16>, chunks * a.B, 16 * 32, 0, s, a, weight, add, row_weight, chunks));
   D3TOM_LAUNCH_CHECK(ctx);
   return D3TOM_OK;
 }

@@ -38,6 +38,8 @@ __global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const Cac
   const size_t pitch = (size_t)a.kv_heads * dh;
   grid_dependency_enter();
   const CachedRun run = cached_run(a, blockIdx.x);
+  cached_write_empty<T>(a, threadIdx.x, kThreads);
+  if (threadIdx.x == 0) cached_write_join(a, run, blockIdx.x);
   CachedWalk walk;
   walk.start(a, run);
   CachedSegment s;
@@ -134,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const Cac
     if (lane < RT) ml_s[warp][lane] = make_float2(m, l);
     __syncthreads();
     // ---- the CTA's: into the output, or into this CTA's place for parts
-    float* part = a.part + ((size_t)blockIdx.x * 2 + s.slot) * RT * (dh + 2);
+    float* part = a.part + ((size_t)blockIdx.x * 2 + s.slot) * cached_part_stride(a);
     for (int i = threadIdx.x; i < s.rows * dh; i += kThreads) {
       const int r = i / dh, d = i - r * dh;
       float mm = ml_s[0][r].x;

@@ -204,23 +204,34 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     }
   } else if (warp == S::kSoftmaxWarps + 2) {
     // ------------------------------------------------------------ Q rows, 128-byte swizzle, a segment ahead
+    cached_write_empty<__nv_bfloat16>(a, lane, 32);
     bool ok = true;
     for (int seg = 0; ok && walk.next(a, s); ++seg) {
       const int qb = S::kQBufs == 2 ? seg & 1 : 0;
       if (seg >= S::kQBufs)
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&q_empty[qb], (uint32_t)(seg / S::kQBufs - 1) & 1u, abort_flag, a.dev_status));
       if (!ok) break;
-      constexpr int kChunks = DH / 8;                   // 16-byte pieces of a row
-      for (int i = lane; i < N * kChunks; i += 32) {
-        const int r = i / kChunks, c = i % kChunks;
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
-        if (r < s.rows) w = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (size_t)cached_row_index(a, s, r) * DH)[c];
-        *reinterpret_cast<uint4*>(q_s + qb * S::kQBytes + (c / 8) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = w;
+      constexpr int kChunks = DH / 8, kAhead = 8;       // 16-byte pieces of a row; loads in flight per lane
+      for (int i0 = lane; i0 < N * kChunks; i0 += 32 * kAhead) {
+        uint4 w[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int r = (i0 + u * 32) / kChunks, c = (i0 + u * 32) % kChunks;
+          w[u] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < s.rows) w[u] = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (size_t)cached_row_index(a, s, r) * DH)[c];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int r = (i0 + u * 32) / kChunks, c = (i0 + u * 32) % kChunks;
+          if (r < N) *reinterpret_cast<uint4*>(q_s + qb * S::kQBytes + (c / 8) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = w[u];
+        }
       }
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&q_full[qb]);
+      if (seg == 0 && lane == 0) cached_write_join(a, run, blockIdx.x);
     }
+    if (run.w0 >= run.w1 && lane == 0) cached_write_join(a, run, blockIdx.x);
   } else {
     // ------------------------------------------------------------ softmax and epilogue
     const int quarter = warp & 3, group = warp >> 2, col0 = group * kCols;
@@ -351,7 +362,7 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         if (lane < kSum) red_s[quarter * N + col0 + i0 + lane] = sum;
       }
       ptx::named_sync(bar, 128);
-      float* part = a.part + ((size_t)blockIdx.x * 2 + s.slot) * N * (DH + 2);
+      float* part = a.part + ((size_t)blockIdx.x * 2 + s.slot) * (N * (DH + 2));
       if (gt < kCols) {
         const float* r = red_s + col0 + gt;
         const float sum = (r[0] + r[N]) + (r[2 * N] + r[3 * N]);

@@ -120,6 +120,50 @@ struct CachedWalk {
   }
 };
 
+// Where a CTA keeps its part of an item: O of the tile's rows, then M of all rows, then l.
+__device__ __forceinline__ size_t cached_part_stride(const CachedArgs& a) {
+  return ((size_t)a.tile_rows * (a.dh + 2) + 3) & ~(size_t)3;
+}
+
+// What the join has to do for a run whose first segment is the end of an item: written by one thread per CTA.
+struct CachedJoin {
+  int first, n;                 // the item's first part (2 * CTA + slot); CTAs that have a part; 0: nothing to join
+  int lo, rows, kv_head, row0, pad0, pad1;
+};
+__device__ __forceinline__ void cached_write_join(const CachedArgs& a, const CachedRun& run, int cta) {
+  CachedJoin j = {};
+  CachedWalk walk;
+  walk.start(a, run);
+  CachedSegment s;
+  if (walk.next(a, s) && s.t0 > 0 && s.t1 == walk.tiles) {
+    const long long begin = run.w0 - s.t0;
+    int c0 = (int)(begin * run.ctas / run.total);
+    while (cached_run_begin(run.total, run.ctas, c0) > begin) --c0;
+    while (cached_run_begin(run.total, run.ctas, c0 + 1) <= begin) ++c0;
+    j.first = 2 * c0 + (cached_run_begin(run.total, run.ctas, c0) == begin ? 0 : 1);
+    j.n = cta - c0 + 1;
+    j.lo = s.lo; j.rows = s.rows; j.kv_head = s.kv_head; j.row0 = s.row0;
+  }
+  int4* dst = reinterpret_cast<int4*>(a.joins) + 2 * cta;
+  dst[0] = make_int4(j.first, j.n, j.lo, j.rows);
+  dst[1] = make_int4(j.kv_head, j.row0, 0, 0);
+}
+
+// What no run has: zeros for the rows of requests without slots, and the word on lengths that do not fit.  `threads` threads of
+// every CTA, this one the `tid`-th of them.
+template <typename T>
+__device__ __forceinline__ void cached_write_empty(const CachedArgs& a, int tid, int threads) {
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+    const CachedRequest r = cached_request(a, b);
+    const int raw = a.length[b];
+    if (tid == 0 && (raw < 0 || raw > a.cap)) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
+    if (r.len > 0) continue;
+    T* out = static_cast<T*>(a.out) + (size_t)r.lo * a.H * a.dh;
+    const size_t count = (size_t)r.n * a.H * a.dh;
+    for (size_t i = tid; i < count; i += threads) out[i] = Storage<T>::from_float(0.f);
+  }
+}
+
 // The rank of row x query head f of a request among all [total_rows * H]: packed row * H + query head.
 __device__ __forceinline__ int cached_row_index(const CachedArgs& a, const CachedSegment& s, int r) {
   const int f = s.row0 + r, i = f / a.group;

@@ -34,6 +34,7 @@ struct d3tom_ctx {
   int* gemm_split_counters;     // [2 * sm_count] slices arrived per tile (similarity: and shares done / left behind); zero between launches
   float* attn_part_ws;          // [sm_count][2][128 + 2][128] fp32: O tile and (m, l) of an attention item's later key tiles
   int* attn_part_flags;         // [sm_count][2][4] one word per (CTA, query tile, warp); zero between launches
+  int* cached_joins;            // [3 * sm_count][8] work items that several CTAs share (cache_walk.cuh)
   int* dev_status;              // device status word
   int vis_stride;               // row stride of score_scratch (floats)
 };
@@ -241,7 +242,8 @@ struct CachedArgs {
   int pages, page_size, max_pages, cap;   // cap: slots a request can have in this call
   float scale_log2;             // softmax_scale * log2(e)
   float* scores; float2* lse; int score_stride;   // [total_rows][H][score_stride] raw q.k and [total_rows][H] (M, l); null without weights
-  float* part;                  // [ctas][2][tile_rows][dh + 2]: tiles of a work item that several CTAs share
+  float* part;                  // [ctas][2] parts of work items that several CTAs share (cache_walk.cuh)
+  int* joins;                   // [ctas][8] what the join has to do
   int tile_rows, ctas;          // set by the launcher
   int* dev_status;
 };
