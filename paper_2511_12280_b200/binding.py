@@ -154,6 +154,13 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _raw_stream(stream, device: int) -> int:
+    """The given stream, or the current one of the context's device (which need not be the current device)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
 def _dt(t: torch.Tensor) -> int:
     if t.dtype == torch.bfloat16:
         return BF16
@@ -308,7 +315,7 @@ class Context:
     # -------------------------------------------------------------- a K/V cache in pages
     def d3tom_rope(self, spec, q, k, positions, rows, kv_heads, q_out, k_out, inverse=False, stream=None):
         _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _ptr(q), _ptr(k), _ptr(positions), rows, kv_heads,
-                                 int(inverse), _ptr(q_out), _ptr(k_out), _stream(stream)), "d3tom_rope")
+                                 int(inverse), _ptr(q_out), _ptr(k_out), _raw_stream(stream, self.device)), "d3tom_rope")
 
     def d3tom_cache_append(self, cache, spec, q, k, v, positions, tokens, first_weight, cu_rows, B, total_rows, q_out,
                            stream=None):
@@ -316,16 +323,16 @@ class Context:
             raise TypeError("rows and cache are of one storage type")
         _check(load().d3tom_cache_append(self._h, cache.dt, cache.ref, None if spec is None else C.byref(spec), _ptr(q), _ptr(k),
                                          _ptr(v), _ptr(positions), _ptr(tokens), _ptr(first_weight), _ptr(cu_rows), B,
-                                         total_rows, _ptr(q_out), _stream(stream)), "d3tom_cache_append")
+                                         total_rows, _ptr(q_out), _raw_stream(stream, self.device)), "d3tom_cache_append")
 
     def d3tom_attn_cached(self, cache, q, cu_rows, B, total_rows, max_rows, max_length, softmax_scale, mode, row_weight, out,
                           stream=None):
         if cache.dt != _dt(q) or cache.dt != _dt(out):
             raise TypeError("rows and cache are of one storage type")
         _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _ptr(q), _ptr(cu_rows), B, total_rows, max_rows,
-                                        max_length, softmax_scale, mode, _ptr(row_weight), _ptr(out), _stream(stream)),
+                                        max_length, softmax_scale, mode, _ptr(row_weight), _ptr(out), _raw_stream(stream, self.device)),
                "d3tom_attn_cached")
 
     def d3tom_cache_evict(self, cache, budget, protect_from, B, max_length, length_out, stream=None):
         _check(load().d3tom_cache_evict(self._h, cache.dt, cache.ref, _ptr(budget), _ptr(protect_from), B, max_length,
-                                        _ptr(length_out), _stream(stream)), "d3tom_cache_evict")
+                                        _ptr(length_out), _raw_stream(stream, self.device)), "d3tom_cache_evict")

@@ -462,14 +462,23 @@ static int make_rope_table(const d3tom_rope_spec* sp, int dh, RopeTable* t) {
   }
   if (n < 1 || n > 64) return D3TOM_ERR_INVALID_ARG;
   t->pairs = n; t->axes = sp->axes; t->neighbours = sp->pairing == D3TOM_PAIR_NEIGHBOURS;
-  for (int a = 0, first = 0; a < sp->axes; first += sp->section[a], ++a)
-    for (int i = first; i < first + sp->section[a]; ++i) {
-      const double e = sp->ladder == D3TOM_LADDER_PER_AXIS ? (double)(i - first) / sp->section[a] : (double)i / n;
-      // theta^-e <= 1 radian, a part of a turn below 1/6: as a 64-bit fraction the product with any position wraps
-      // around at whole turns, which is what an angle does
-      t->turn[i] = (unsigned long long)(pow(sp->theta, -e) * (18446744073709551616.0 / 6.283185307179586476925));
+  // theta^-e <= 1 radian, a part of a turn below 1/6: as a 64-bit fraction the product with any position wraps around at whole
+  // turns, which is what an angle does.  The powers are products in the 64-bit mantissa of long double (64 calls of pow took 2 us
+  // of every call).
+  const long double unit = 18446744073709551616.0L / 6.283185307179586476925286766559005768L;
+  long double shared = unit;
+  const long double step_shared = sp->ladder == D3TOM_LADDER_SHARED ? powl(sp->theta, -1.0L / n) : 1.0L;
+  for (int a = 0, i = 0; a < sp->axes; ++a) {
+    long double own = unit;
+    const long double step_own =
+        sp->ladder == D3TOM_LADDER_PER_AXIS && sp->section[a] > 0 ? powl(sp->theta, -1.0L / sp->section[a]) : 1.0L;
+    for (int j = 0; j < sp->section[a]; ++j, ++i) {
+      t->turn[i] = (unsigned long long)(sp->ladder == D3TOM_LADDER_PER_AXIS ? own : shared);
       t->axis[i] = (unsigned char)a;
+      own *= step_own;
+      shared *= step_shared;
     }
+  }
   return D3TOM_OK;
 }
 
@@ -570,7 +579,7 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
   if (st != D3TOM_OK) return st;
   const bool tensor = dt == D3TOM_BF16 && !ctx->reference_kernels;
   if (tensor && cache->page_size % 8 != 0) return D3TOM_ERR_UNSUPPORTED;
-  if ((long long)total_rows * ctx->lim.heads > 0x7fffffffll) return D3TOM_ERR_UNSUPPORTED;
+  if ((long long)total_rows * ctx->lim.heads > 0x7fffffffll - 128) return D3TOM_ERR_UNSUPPORTED;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return D3TOM_ERR_CUDA;
   CachedArgs a = {};

@@ -24,19 +24,19 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const CachedArgs 
   const size_t first = (size_t)j0.x, rest = (size_t)(j0.x / 2) * 2;
   auto part = [&](int i) { return a.part + (i == 0 ? first : rest + 2 * (size_t)i) * stride; };
   const size_t at_m = (size_t)a.tile_rows * dh + r, at_l = at_m + a.tile_rows;
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, part(i)[at_m]);
+  // (M, l) of the first 32 parts stay in registers: one round trip to L2 less where there are no more
+  float m0 = -INFINITY, l0 = 0.f;
+  if (lane < n) { m0 = part(lane)[at_m]; l0 = part(lane)[at_l]; }
+  float m = m0;
+  for (int i = lane + 32; i < n; i += 32) m = fmaxf(m, part(i)[at_m]);
   m = warp_max(m);
   float l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i0 = 0; i0 < n; i0 += 32) {
     const int i = i0 + lane;
-    float f = 0.f;
-    if (i < n) {
-      const float* p = part(i);
-      f = ptx::ex2(p[at_m] - m);
-      l += p[at_l] * f;
-    }
+    if (i0 > 0 && i < n) { m0 = part(i)[at_m]; l0 = part(i)[at_l]; }
+    const float f = i < n ? ptx::ex2(m0 - m) : 0.f;
+    l += i < n ? l0 * f : 0.f;
     const int many = min(32, n - i0);
 #pragma unroll 8
     for (int k = 0; k < many; ++k) {

@@ -16,7 +16,7 @@
 // each term at most, unbiased), as in the other attention kernels.
 //
 //   warps 0 .. 3 (N = 128: 0 .. 7, a half of the columns each)  softmax and epilogue, a key / a number of O per thread
-//   then one warp each: TMA producer, MMA issue, Q rows into shared memory
+//   then one warp each: MMA issue, Q rows into shared memory, TMA producer of K, TMA producer of V
 // One CTA per SM walks its run of key tiles (cache_walk.cuh).  Every wait is bounded; after one that ran out the softmax
 // warps go through the rest of their run without waiting (their barriers need all of them), the other warps stop.
 #include "cache_walk.cuh"
@@ -28,16 +28,21 @@ template <int DH, int N> struct Shape {
   static constexpr int kGroups = N > 64 ? 2 : 1;            // softmax warpgroups
   static constexpr int kCols = N / kGroups;                 // columns per softmax thread
   static constexpr int kSoftmaxWarps = 4 * kGroups;
-  static constexpr int kThreads = (kSoftmaxWarps + 3) * 32;
+  static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
   static constexpr int kSlotBytes = kKeyTile * DH * 2;
+  // CTAs per SM: a tile of head_dim 64 has half the bytes but as long a way through softmax (some 1900 cycles, against 1400 for its
+  // bytes), so two of them run side by side where their shared memory allows (64 requests, up to 8192 slots, 32 / 16 heads x 64:
+  // 249 -> 205 us; blocks of 32 rows 60 -> 51)
+  static constexpr int kPerSm = DH == 64 && N <= 32 ? 2 : 1;
   static constexpr int kQBufs = DH * N >= 128 * 128 ? 1 : 2;
-  static constexpr int kSlots = (N <= 32 ? 6 : N == 64 ? 5 : 4) * (128 / DH);
+  static constexpr int kSlots = DH == 128 ? (N <= 32 ? 6 : 4) : N == 16 ? 6 : N == 32 ? 4 : N == 64 ? 10 : 8;
+  static_assert(kSlots % 2 == 0, "K tiles in the even slots, V tiles in the odd ones: no slot has two producers");
   static constexpr int kQBytes = N * DH * 2;
   static constexpr int kPBytes = N * kKeyTile * 2;
   static constexpr int kFloats = N * 7;                     // reference, factor, four warps' values, row numbers
   static constexpr int kBars = 2 * kSlots + 2 * 2 + 2 + 2;
   static constexpr int kBytes = 1024 + kSlots * kSlotBytes + kQBufs * kQBytes + kPBytes + kFloats * 4 + kBars * 8 + 64;
-  static_assert(kBytes <= 227 * 1024, "shared memory of an SM");
+  static_assert(kPerSm * (kBytes + 1024) <= 228 * 1024, "shared memory of an SM");
   static constexpr uint32_t kTmemCols = N == 16 ? 64 : 4 * N;   // S twice and O: 3 N, as a power of two
 };
 
@@ -58,7 +63,7 @@ __device__ __forceinline__ float lane_sums(float (&v)[C]) {
 }
 
 template <int DH, int N>
-__global__ void __launch_bounds__(Shape<DH, N>::kThreads, 1)
+__global__ void __launch_bounds__(Shape<DH, N>::kThreads, Shape<DH, N>::kPerSm)
 attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const CachedArgs a,
                       const int box) {
   using S = Shape<DH, N>;
@@ -106,11 +111,15 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
   walk.start(a, run);
   CachedSegment s;
 
-  if (warp == S::kSoftmaxWarps) {
-    // ------------------------------------------------------------ TMA producer: a lane per page part
-    if (lane == 0) { ptx::prefetch_tensormap(&tmap_k); ptx::prefetch_tensormap(&tmap_v); }
+  if (warp >= S::kSoftmaxWarps + 2) {
+    // ------------------------------------------------------------ TMA producers, one for K and one for V: a lane per page part
+    const int kind = warp - (S::kSoftmaxWarps + 2);
+    const CUtensorMap* tmap = kind == 0 ? &tmap_k : &tmap_v;
+    if (lane == 0) ptx::prefetch_tensormap(tmap);
     const int boxes = kKeyTile / box, outside = a.pages * a.page_size;
-    int ring = 0, issued = 0, tile = 0;
+    // a cache that is read once need not push the scores out of L2
+    const uint64_t policy = ptx::l2_policy(a.read_once != 0);
+    int ring = kind, issued = 0, tile = 0;
     uint32_t phase = 1;                                 // of the ring's `empty` barriers: the first round finds them so
     bool ok = true;
     while (ok && walk.next(a, s)) {
@@ -122,35 +131,34 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         return at < 0 ? -1 : (int)at;
       };
       int row = find(s.t0);
-      for (int t = s.t0; t < s.t1 && ok; ++t, ++tile) {
+      for (int t = s.t0; t < s.t1; ++t, ++tile) {
         const uint32_t bad = __ballot_sync(0xffffffffu, row < 0);
         if (row < 0) { row = outside; atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG); }
-        if (lane == 0) bad_boxes[tile & 7] = bad;
         const int next_row = t + 1 < s.t1 ? find(t + 1) : outside;
+        ok = __all_sync(0xffffffffu, ptx::mbar_wait(&kv_empty[ring], phase, abort_flag, a.dev_status));
+        if (!ok) break;
+        if (lane == 0 && kind == 0) bad_boxes[tile & 7] = bad;   // (at most seven tiles ahead of the softmax warps)
+        if (lane == 0) ptx::mbar_arrive_expect_tx(&kv_full[ring], S::kSlotBytes);
+        __syncwarp();
+        if (lane < boxes)
 #pragma unroll
-        for (int kind = 0; kind < 2; ++kind) {
-          ok = __all_sync(0xffffffffu, ptx::mbar_wait(&kv_empty[ring], phase, abort_flag, a.dev_status));
-          if (!ok) break;
-          if (lane == 0) ptx::mbar_arrive_expect_tx(&kv_full[ring], S::kSlotBytes);
-          __syncwarp();
-          if (lane < boxes)
-#pragma unroll
-            for (int hf = 0; hf < DH / 64; ++hf)
-              ptx::tma_load_2d(kv_s + ring * S::kSlotBytes + hf * kHalfBytes + lane * box * 128, kind == 0 ? &tmap_k : &tmap_v,
-                               &kv_full[ring], s.kv_head * DH + hf * 64, row);
-          ++issued;
-          if (++ring == kSlots) { ring = 0; phase ^= 1u; }
-        }
+          for (int hf = 0; hf < DH / 64; ++hf)
+            ptx::tma_load_2d_hint(kv_s + ring * S::kSlotBytes + hf * kHalfBytes + lane * box * 128, tmap, &kv_full[ring],
+                                  s.kv_head * DH + hf * 64, row, policy);
+        ++issued;
+        ring += 2;
+        if (ring >= kSlots) { ring -= kSlots; phase ^= 1u; }
         row = next_row;
       }
     }
     if (!ok) {                                          // copies under way land before the CTA leaves
-      for (int i = 0; i < kSlots && i < issued; ++i) {
-        if (--ring < 0) { ring = kSlots - 1; phase ^= 1u; }
+      for (int i = 0; i < kSlots / 2 && i < issued; ++i) {
+        ring -= 2;
+        if (ring < 0) { ring += kSlots; phase ^= 1u; }
         ptx::mbar_wait(&kv_full[ring], phase ^ 1u, abort_flag, a.dev_status);
       }
     }
-  } else if (warp == S::kSoftmaxWarps + 1) {
+  } else if (warp == S::kSoftmaxWarps) {
     // ------------------------------------------------------------ MMA issue
     if (ptx::elect_one()) {
       constexpr uint32_t idesc_qk = ptx::idesc_bf16_f32(kKeyTile, N, 0, 0);    // both along dh
@@ -202,7 +210,7 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       }
       if (ok && tile > 0) issue_pv(tile - 1);
     }
-  } else if (warp == S::kSoftmaxWarps + 2) {
+  } else if (warp == S::kSoftmaxWarps + 1) {
     // ------------------------------------------------------------ Q rows, 128-byte swizzle, a segment ahead
     cached_write_empty<__nv_bfloat16>(a, lane, 32);
     bool ok = true;
@@ -409,11 +417,12 @@ int launch(d3tom_ctx* ctx, CachedArgs a, cudaStream_t s) {
   while (a.page_size % box != 0) box >>= 1;
   CUtensorMap tk, tv;
   const uint64_t rows = (uint64_t)a.pages * a.page_size, cols = (uint64_t)a.kv_heads * DH;
-  int r = make_tmap_bf16_2d(&tk, a.k, rows, cols, cols, (uint32_t)box);
-  if (r == 0) r = make_tmap_bf16_2d(&tv, a.v, rows, cols, cols, (uint32_t)box);
+  int r = make_tmap_bf16_2d(&tk, a.k, rows, cols, cols, (uint32_t)box, 64, DH == 64);
+  if (r == 0) r = make_tmap_bf16_2d(&tv, a.v, rows, cols, cols, (uint32_t)box, 64, DH == 64);
   if (r != 0) { ctx->last_cuda_error = r; return D3TOM_ERR_CUDA; }
   a.tile_rows = N;
-  a.ctas = ctx->sm_count;
+  a.read_once = (long long)a.max_rows * a.group <= N;
+  a.ctas = Sh::kPerSm * ctx->sm_count;
   auto kernel = attn_cached_tc_kernel<DH, N>;
   D3TOM_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes));
   D3TOM_CUDA_TRY(ctx, launch_serialized(kernel, a.ctas, Sh::kThreads, Sh::kBytes, s, tk, tv, a, box));

@@ -26,7 +26,7 @@ __device__ __forceinline__ CachedRequest cached_request(const CachedArgs& a, int
   return r;
 }
 __device__ __forceinline__ int cached_row_tiles(const CachedArgs& a, int n) {
-  return (int)(((long long)n * a.group + a.tile_rows - 1) / a.tile_rows);
+  return (n * a.group + a.tile_rows - 1) / a.tile_rows;     // (all rows x heads of a call fit 31 bits, less a tile)
 }
 __device__ __forceinline__ int cached_key_tiles(int len) { return (len + kKeyTile - 1) / kKeyTile; }
 __device__ __forceinline__ long long cached_work(const CachedArgs& a, const CachedRequest& r) {
@@ -38,7 +38,11 @@ struct CachedRun {
   long long w0, w1, base, total;   // tiles [w0, w1) of `total`; the first tile of request b
   int b, ctas;                     // ctas that have work
 };
-__device__ __forceinline__ long long cached_run_begin(long long total, int ctas, int c) { return total * c / ctas; }
+// (a 64-bit division is some 300 cycles on the way to a CTA's first load: 32 bits where they do)
+__device__ __forceinline__ long long cached_div(long long x, int y) {
+  return (x >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+}
+__device__ __forceinline__ long long cached_run_begin(long long total, int ctas, int c) { return cached_div(total * c, ctas); }
 
 // Whole warp; the same answer in all lanes.
 __device__ __forceinline__ CachedRun cached_run(const CachedArgs& a, int cta) {
@@ -106,7 +110,7 @@ struct CachedWalk {
     if (w >= w_end) return false;
     while (w >= base + work) { base += work; ++b; enter(a); }
     const long long rel = w - base;
-    const int item = (int)(rel / tiles);
+    const int item = (int)cached_div(rel, tiles);
     s.t0 = (int)(rel - (long long)item * tiles);
     s.t1 = (int)min((long long)tiles, s.t0 + (w_end - w));
     s.whole = s.t0 == 0 && s.t1 == tiles;

@@ -244,7 +244,7 @@ struct CachedArgs {
   float* scores; float2* lse; int score_stride;   // [total_rows][H][score_stride] raw q.k and [total_rows][H] (M, l); null without weights
   float* part;                  // [ctas][2] parts of work items that several CTAs share (cache_walk.cuh)
   int* joins;                   // [ctas][8] what the join has to do
-  int tile_rows, ctas;          // set by the launcher
+  int tile_rows, ctas, read_once;   // set by the launcher; read_once: no item shares its keys with another
   int* dev_status;
 };
 int launch_attn_cached_simt(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
