@@ -11,8 +11,11 @@
 
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = kWarps * 32;
+// Warps per CTA and CTAs per SM for RT rows per tile: one row needs the registers for its loads, eight rows for their sums.
+template <int RT> struct SimtShape {
+  static constexpr int kWarps = RT == 8 ? 4 : 8;
+  static constexpr int kCtas = RT == 8 ? 3 : RT == 1 ? 1 : 2;
+};
 
 template <typename T> __device__ __forceinline__ float4 load4(const T* p);
 template <> __device__ __forceinline__ float4 load4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
@@ -24,7 +27,8 @@ template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bf
 
 // RT rows per tile; a key's numbers are split over LPK lanes
 template <typename T, int RT, int LPK>
-__global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const CachedArgs a) {
+__global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCtas) attn_cached_simt_kernel(const CachedArgs a) {
+  constexpr int kWarps = SimtShape<RT>::kWarps, kThreads = kWarps * 32;
   constexpr int kKeys = 32 / RT;                 // keys per warp and step
   constexpr int kSide = 32 / LPK;                // .. side by side
   constexpr int kPasses = kKeys / kSide;         // .. one after the other
@@ -59,6 +63,7 @@ __global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const Cac
     const int end = min(s.len, s.t1 * kKeyTile);
     for (int key0 = s.t0 * kKeyTile + warp * kKeys; key0 < end; key0 += kWarps * kKeys) {
       float val[LPK];
+      float4 vv[kAhead];
       int at = -1;                               // lane i: where key i is (slots of a pool are counted in 31 bits)
       if (lane < kKeys && key0 + lane < end) at = (int)cached_place(table, key0 + lane, a.page_size, a.pages);
       int place[kPasses];
@@ -67,6 +72,10 @@ __global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const Cac
 #pragma unroll
       for (int p0 = 0; p0 < kPasses; p0 += kAhead) {
         float4 kk[kAhead];
+        if (p0 == 0)                             // the first values are under way with the first keys
+#pragma unroll
+          for (int p = 0; p < kAhead; ++p)
+            vv[p] = place[p] >= 0 && has ? load4(vp + (size_t)place[p] * pitch) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int p = 0; p < kAhead; ++p)
           kk[p] = place[p0 + p] >= 0 && has ? load4(kp + (size_t)place[p0 + p] * pitch) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -108,7 +117,7 @@ __global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const Cac
       l += pr;
 #pragma unroll
       for (int p0 = 0; p0 < kPasses; p0 += kAhead) {
-        float4 vv[kAhead];
+        if (p0 > 0)
 #pragma unroll
         for (int p = 0; p < kAhead; ++p)
           vv[p] = place[p0 + p] >= 0 && has ? load4(vp + (size_t)place[p0 + p] * pitch) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -163,16 +172,25 @@ __global__ void __launch_bounds__(kThreads, 3) attn_cached_simt_kernel(const Cac
   }
 }
 
-template <typename T, int LPK>
-int launch(d3tom_ctx* ctx, d3tom_dtype dt, CachedArgs a, cudaStream_t s) {
-  const long long rows = (long long)a.max_rows * a.group;
-  a.ctas = 3 * ctx->sm_count;
-  a.tile_rows = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8;
-  auto kernel = a.tile_rows == 1 ? attn_cached_simt_kernel<T, 1, LPK> : a.tile_rows == 2 ? attn_cached_simt_kernel<T, 2, LPK>
-              : a.tile_rows == 4 ? attn_cached_simt_kernel<T, 4, LPK> : attn_cached_simt_kernel<T, 8, LPK>;
-  D3TOM_CUDA_TRY(ctx, launch_serialized(kernel, a.ctas, kThreads, 0, s, a));
+template <typename T, int RT, int LPK>
+int launch_rows(d3tom_ctx* ctx, d3tom_dtype dt, CachedArgs a, cudaStream_t s) {
+  a.ctas = SimtShape<RT>::kCtas * ctx->sm_count;
+  a.tile_rows = RT;
+  D3TOM_CUDA_TRY(ctx, launch_serialized(attn_cached_simt_kernel<T, RT, LPK>, a.ctas, SimtShape<RT>::kWarps * 32, 0, s, a));
   D3TOM_LAUNCH_CHECK(ctx);
   return launch_attn_cached_join(ctx, dt, a, s);
+}
+
+template <typename T, int LPK>
+int launch(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s) {
+  const long long rows = (long long)a.max_rows * a.group;
+  if (rows <= 1) return launch_rows<T, 1, LPK>(ctx, dt, a, s);
+  if (rows <= 2) return launch_rows<T, 2, LPK>(ctx, dt, a, s);
+  // Eight rows share a key's bytes, four make more work items of a small call (us, eight / four: 12 rows x 4 key heads x four
+  // requests up to 2177 slots x 64 26.3 / 22.7; 32 rows x 4 x four of 8000 x 128 158 / 185).  Asked with the longest length there can be.
+  const long long items = (long long)a.B * a.kv_heads * ((rows + 7) / 8) * ceil_div(a.cap, kKeyTile);
+  if (rows <= 4 || items < 6 * ctx->sm_count) return launch_rows<T, 4, LPK>(ctx, dt, a, s);
+  return launch_rows<T, 8, LPK>(ctx, dt, a, s);
 }
 
 }  // namespace

@@ -18,6 +18,15 @@ template <typename T> __device__ __forceinline__ T rotated_hi(T x, T y, float c,
   return Storage<T>::from_float(Storage<T>::to_float(x) * s + Storage<T>::to_float(y) * c);
 }
 
+// Where a row goes in the pools; -1: nowhere.
+__device__ __forceinline__ long long row_place(const RotateArgs& a, int row) {
+  const int b = find_segment(a.cu_rows, a.B, row);
+  const long long slot = (long long)a.cache.length[b] - a.cu_rows[b + 1] + row;
+  if (slot < 0 || slot >= (long long)a.cache.max_pages * a.cache.page_size) return -1;
+  const int p = (int)slot / a.cache.page_size, page = a.cache.page_table[(size_t)b * a.cache.max_pages + p];
+  return page < 0 || page >= a.cache.pages ? -1 : (long long)page * a.cache.page_size + ((int)slot - p * a.cache.page_size);
+}
+
 // One block per row (blockIdx.x); gridDim.y blocks share its heads.  kVector: units of 16 bytes (pairs of halves: 2 x 16, where
 // the number of pairs is a multiple of the vector); otherwise a pair or a copied number at a time.
 template <typename T, bool kVector>
@@ -30,12 +39,7 @@ rotate_rows_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, cons
   long long place = -1;                          // where the row goes in the pools
   if (to_cache) {
     if (row >= a.cu_rows[a.B]) return;           // (the whole block)
-    const int b = find_segment(a.cu_rows, a.B, row);
-    const long long slot = (long long)a.cache.length[b] - a.cu_rows[b + 1] + row;
-    if (slot >= 0 && slot < (long long)a.cache.max_pages * a.cache.page_size) {
-      const int p = (int)slot / a.cache.page_size, page = a.cache.page_table[(size_t)b * a.cache.max_pages + p];
-      if (page >= 0 && page < a.cache.pages) place = (long long)page * a.cache.page_size + ((int)slot - p * a.cache.page_size);
-    }
+    place = row_place(a, row);
     if (place < 0 && tid == 0) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
     if (tid == 0 && blockIdx.y == 0 && place >= 0) {
       if (a.cache.weight != nullptr) a.cache.weight[place] = a.first_weight != nullptr ? a.first_weight[row] : 0.f;
@@ -126,9 +130,138 @@ rotate_rows_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, cons
   }
 }
 
+// Heads that are rotated whole (2 pairs = dh): a warp takes a row, or a part of its heads where there are few rows.  U lanes have a head, a
+// lane always the same pairs of every head, so their cosines and sines stay in registers; four heads' loads are under way
+// at a time, the first ones before the angles are known.  4288 rows x 64 heads x 128: 27.8 us with the kernel above (angles from
+// shared memory for every unit, a barrier per row).
+constexpr int kHeadWarps = 4;
+constexpr int kHeadBatch = 4;
+
+template <typename T, bool kNeighbours, int U>
+__global__ void __launch_bounds__(kHeadWarps * 32)
+rotate_heads_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, const bool to_cache, const int parts) {
+  constexpr int kVec = Storage<T>::kVec, kPairs = kNeighbours ? kVec / 2 : kVec, kHeads = 32 / U;
+  const int lane = threadIdx.x & 31, w = blockIdx.x * kHeadWarps + (threadIdx.x >> 5);
+  const int row = w / parts, part = w - row * parts;
+  if (row >= a.rows) return;
+  grid_dependency_enter();
+  if (to_cache && row >= a.cu_rows[a.B]) return;
+  const int dh = a.dh, heads = a.H + a.kv_heads, step = parts * kHeads, at = (lane % U) * kVec, half = dh / 2;
+  const size_t width = (size_t)a.kv_heads * dh;
+  const T* q = static_cast<const T*>(a.q) + (size_t)row * a.H * dh + at;
+  const T* k = static_cast<const T*>(a.k) + (size_t)row * width + at;
+  uint4 lo[kHeadBatch], hi[kHeadBatch];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int j = 0; j < kHeadBatch; ++j) {
+      const int h = h0 + j * step;
+      if (h < heads) {
+        const T* src = h < a.H ? q + (size_t)h * dh : k + (size_t)(h - a.H) * dh;
+        lo[j] = *reinterpret_cast<const uint4*>(src);
+        if (!kNeighbours) hi[j] = *reinterpret_cast<const uint4*>(src + half);
+      }
+    }
+  };
+  int h = part * kHeads + lane / U;
+  load(h);
+  // the angles: lane i has pairs i and i + 32, then every lane collects those of its place in a head
+  float c[2] = {1.f, 1.f}, s[2] = {0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int pr = lane + j * 32;
+    if (pr < t.pairs) {
+      const long long pos = a.positions[(size_t)row * t.axes + t.axis[pr]];
+      const int32_t x = (int32_t)(((unsigned long long)pos * t.turn[pr]) >> 32);
+      sincospif((float)x * 4.656612873077392578125e-10f, &s[j], &c[j]);
+      if (a.inverse) s[j] = -s[j];
+    }
+  }
+  float cs[kPairs], sn[kPairs];
+#pragma unroll
+  for (int e = 0; e < kPairs; ++e) {
+    const int pr = (lane % U) * kPairs + e;
+    const float c0 = __shfl_sync(0xffffffffu, c[0], pr & 31), c1 = __shfl_sync(0xffffffffu, c[1], pr & 31);
+    const float s0 = __shfl_sync(0xffffffffu, s[0], pr & 31), s1 = __shfl_sync(0xffffffffu, s[1], pr & 31);
+    cs[e] = pr < 32 ? c0 : c1;
+    sn[e] = pr < 32 ? s0 : s1;
+  }
+  long long place = row;                         // of the row in the keys' destination
+  if (to_cache) {
+    place = row_place(a, row);
+    if (part == 0 && lane == 0) {
+      if (place < 0) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
+      else {
+        if (a.cache.weight != nullptr) a.cache.weight[place] = a.first_weight != nullptr ? a.first_weight[row] : 0.f;
+        if (a.tokens != nullptr) a.cache.token[place] = a.tokens[row];
+      }
+    }
+  }
+  T* q_out = static_cast<T*>(a.q_out) + (size_t)row * a.H * dh + at;
+  T* k_out = static_cast<T*>(to_cache ? a.cache.k : a.k_out) + (size_t)(place < 0 ? 0 : place) * width + at;
+  for (; h < heads; h += kHeadBatch * step) {
+    if (h != part * kHeads + lane / U) load(h);
+#pragma unroll
+    for (int j = 0; j < kHeadBatch; ++j) {
+      const int hj = h + j * step;
+      if (hj >= heads || (hj >= a.H && place < 0)) continue;
+      T* dst = hj < a.H ? q_out + (size_t)hj * dh : k_out + (size_t)(hj - a.H) * dh;
+      float x[kVec], y[kVec];
+      Storage<T>::load(reinterpret_cast<const T*>(&lo[j]), x);
+      if constexpr (kNeighbours) {
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+          const float p = x[2 * e], r = x[2 * e + 1];
+          y[2 * e] = p * cs[e] - r * sn[e];
+          y[2 * e + 1] = p * sn[e] + r * cs[e];
+        }
+        Storage<T>::store(dst, y);
+      } else {
+        Storage<T>::load(reinterpret_cast<const T*>(&hi[j]), y);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+          const float p = x[e] * cs[e] - y[e] * sn[e];
+          y[e] = x[e] * sn[e] + y[e] * cs[e];
+          x[e] = p;
+        }
+        Storage<T>::store(dst, x);
+        Storage<T>::store(dst + half, y);
+      }
+    }
+  }
+  if (a.v != nullptr && place >= 0) {
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + (size_t)row * width);
+    uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.cache.v) + (size_t)place * width);
+    const int units = (int)(width / kVec);
+    for (int u = part * 32 + lane; u < units; u += kHeadBatch * 32 * parts) {
+#pragma unroll
+      for (int j = 0; j < kHeadBatch; ++j) if (u + j * 32 * parts < units) lo[j] = src[u + j * 32 * parts];
+#pragma unroll
+      for (int j = 0; j < kHeadBatch; ++j) if (u + j * 32 * parts < units) dst[u + j * 32 * parts] = lo[j];
+    }
+  }
+}
+
+template <typename T, bool kNeighbours, int U>
+int launch_heads(d3tom_ctx* ctx, const RotateArgs& a, const RopeTable& t, bool to_cache, cudaStream_t s) {
+  const int steps = ceil_div(a.H + a.kv_heads, 32 / U), want = ceil_div(24 * ctx->sm_count, a.rows);
+  const int parts = want < steps ? want : steps;
+  D3TOM_CUDA_TRY(ctx, launch_serialized(rotate_heads_kernel<T, kNeighbours, U>, (int)(((long long)a.rows * parts + kHeadWarps - 1) / kHeadWarps),
+                                        kHeadWarps * 32, 0, s, a, t, to_cache, parts));
+  D3TOM_LAUNCH_CHECK(ctx);
+  return D3TOM_OK;
+}
+
 template <typename T>
 int launch(d3tom_ctx* ctx, const RotateArgs& a, const RopeTable& t, bool to_cache, cudaStream_t s) {
   constexpr int kVec = Storage<T>::kVec;
+  const int lanes = 2 * t.pairs != a.dh ? 0 : t.neighbours ? a.dh / kVec : t.pairs % kVec == 0 ? t.pairs / kVec : 0;   // of a whole head
+  switch (lanes) {
+    case 4: if (!t.neighbours) return launch_heads<T, false, 4>(ctx, a, t, to_cache, s); break;
+    case 8: return t.neighbours ? launch_heads<T, true, 8>(ctx, a, t, to_cache, s) : launch_heads<T, false, 8>(ctx, a, t, to_cache, s);
+    case 16: return t.neighbours ? launch_heads<T, true, 16>(ctx, a, t, to_cache, s) : launch_heads<T, false, 16>(ctx, a, t, to_cache, s);
+    case 32: if (t.neighbours) return launch_heads<T, true, 32>(ctx, a, t, to_cache, s); break;
+    default: break;
+  }
   const int units = (a.H + 2 * a.kv_heads) * a.dh / kVec;
   const int want = ceil_div(2 * ctx->sm_count, a.rows), most = ceil_div(units, kThreads);
   const dim3 grid(a.rows, want < 1 ? 1 : want < most ? want : most);
