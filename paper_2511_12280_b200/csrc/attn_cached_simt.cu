@@ -42,12 +42,13 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
   const size_t pitch = (size_t)a.kv_heads * dh;
   grid_dependency_enter();
   const CachedRun run = cached_run(a, blockIdx.x);
-  cached_write_empty<T>(a, threadIdx.x, kThreads);
-  if (threadIdx.x == 0) cached_write_join(a, run, blockIdx.x);
   CachedWalk walk;
   walk.start(a, run);
-  CachedSegment s;
+  CachedSegment s = {};
+  bool head = true;                              // the run's first segment
   while (walk.next(a, s)) {
+    if (head && threadIdx.x == kThreads - 1) cached_write_join(a, run, blockIdx.x, s, walk.tiles);
+    head = false;
     const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
     const T* kp = static_cast<const T*>(a.k) + (size_t)s.kv_head * dh + d0;
     const T* vp = static_cast<const T*>(a.v) + (size_t)s.kv_head * dh + d0;
@@ -170,6 +171,8 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
     }
     __syncthreads();
   }
+  if (head && threadIdx.x == 0) cached_write_join(a, run, blockIdx.x, s, 0);
+  cached_write_empty<T>(a, threadIdx.x, kThreads);
 }
 
 template <typename T, int RT, int LPK>

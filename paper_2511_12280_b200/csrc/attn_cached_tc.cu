@@ -212,10 +212,12 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     }
   } else if (warp == S::kSoftmaxWarps + 1) {
     // ------------------------------------------------------------ Q rows, 128-byte swizzle, a segment ahead
-    cached_write_empty<__nv_bfloat16>(a, lane, 32);
     bool ok = true;
+    CachedSegment head = {};                            // the run's first segment
+    int head_tiles = 0;
     for (int seg = 0; ok && walk.next(a, s); ++seg) {
       const int qb = S::kQBufs == 2 ? seg & 1 : 0;
+      if (seg == 0) { head = s; head_tiles = walk.tiles; }
       if (seg >= S::kQBufs)
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&q_empty[qb], (uint32_t)(seg / S::kQBufs - 1) & 1u, abort_flag, a.dev_status));
       if (!ok) break;
@@ -237,9 +239,9 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&q_full[qb]);
-      if (seg == 0 && lane == 0) cached_write_join(a, run, blockIdx.x);
     }
-    if (run.w0 >= run.w1 && lane == 0) cached_write_join(a, run, blockIdx.x);
+    if (lane == 0) cached_write_join(a, run, blockIdx.x, head, head_tiles);
+    cached_write_empty<__nv_bfloat16>(a, lane, 32);
   } else {
     // ------------------------------------------------------------ softmax and epilogue
     const int quarter = warp & 3, group = warp >> 2, col0 = group * kCols;

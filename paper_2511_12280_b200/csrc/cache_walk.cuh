@@ -44,16 +44,22 @@ __device__ __forceinline__ long long cached_div(long long x, int y) {
 }
 __device__ __forceinline__ long long cached_run_begin(long long total, int ctas, int c) { return cached_div(total * c, ctas); }
 
-// Whole warp; the same answer in all lanes.
+// Whole warp; the same answer in all lanes.  (One pass over the lengths where a warp's lanes have them all: this lies on every
+// call's way to its first load.)
 __device__ __forceinline__ CachedRun cached_run(const CachedArgs& a, int cta) {
   const int lane = threadIdx.x & 31;
-  long long total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 32) {
-    const int b = b0 + lane;
-    total += b < a.B ? cached_work(a, cached_request(a, b)) : 0;
-  }
+  auto work_of = [&](int b) { return b < a.B ? cached_work(a, cached_request(a, b)) : 0ll; };
+  auto scan = [&](long long v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long t = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += t;
+    }
+    return v;
+  };
+  const long long mine0 = work_of(lane), incl0 = scan(mine0);
+  long long total = __shfl_sync(0xffffffffu, incl0, 31);
+  for (int b0 = 32; b0 < a.B; b0 += 32) total += __shfl_sync(0xffffffffu, scan(work_of(b0 + lane)), 31);
   CachedRun run;
   run.total = total;
   run.ctas = total < a.ctas ? (int)total : a.ctas;
@@ -61,26 +67,21 @@ __device__ __forceinline__ CachedRun cached_run(const CachedArgs& a, int cta) {
   if (cta >= run.ctas) return run;
   run.w0 = cached_run_begin(total, run.ctas, cta);
   run.w1 = cached_run_begin(total, run.ctas, cta + 1);
-  long long before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 32) {
-    const int b = b0 + lane;
-    const long long mine = b < a.B ? cached_work(a, cached_request(a, b)) : 0;
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long t = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += t;
-    }
+  long long before = 0, mine = mine0, incl = incl0;
+  for (int b0 = 0; ; ) {
     const unsigned hit = __ballot_sync(0xffffffffu, before + incl > run.w0);
-    if (hit != 0u) {
+    if (hit != 0u) {                              // (w0 < total: some request has it)
       const int src = __ffs(hit) - 1;
       run.b = b0 + src;
       run.base = before + __shfl_sync(0xffffffffu, incl - mine, src);
       return run;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
+    b0 += 32;
+    if (b0 >= a.B) return run;
+    mine = work_of(b0 + lane);
+    incl = scan(mine);
   }
-  return run;
 }
 
 // The segments of a run, one after the other.
@@ -134,12 +135,10 @@ struct CachedJoin {
   int first, n;                 // the item's first part (2 * CTA + slot); CTAs that have a part; 0: nothing to join
   int lo, rows, kv_head, row0, pad0, pad1;
 };
-__device__ __forceinline__ void cached_write_join(const CachedArgs& a, const CachedRun& run, int cta) {
+// s: the run's first segment, of an item of `tiles` key tiles
+__device__ __forceinline__ void cached_write_join(const CachedArgs& a, const CachedRun& run, int cta, const CachedSegment& s, int tiles) {
   CachedJoin j = {};
-  CachedWalk walk;
-  walk.start(a, run);
-  CachedSegment s;
-  if (walk.next(a, s) && s.t0 > 0 && s.t1 == walk.tiles) {
+  if (run.w0 < run.w1 && s.t0 > 0 && s.t1 == tiles) {
     const long long begin = run.w0 - s.t0;
     int c0 = (int)(begin * run.ctas / run.total);
     while (cached_run_begin(run.total, run.ctas, c0) > begin) --c0;

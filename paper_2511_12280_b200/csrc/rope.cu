@@ -131,16 +131,21 @@ rotate_rows_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, cons
 }
 
 // Heads that are rotated whole (2 pairs = dh): a warp takes a row, or a part of its heads where there are few rows.  U lanes have a head, a
-// lane always the same pairs of every head, so their cosines and sines stay in registers; four heads' loads are under way
-// at a time, the first ones before the angles are known.  4288 rows x 64 heads x 128: 27.8 us with the kernel above (angles from
-// shared memory for every unit, a barrier per row).
+// lane always the same pairs of every head, so their cosines and sines stay in registers; 64 bytes of loads per lane are under
+// way at a time (with 128 a wave of blocks does not fit the SMs), the first ones before the angles are known.  Heads of 128 bf16, us, with
+// the kernel above (angles from shared memory for every unit, a barrier per row) / here: 4288 rows x 64 heads 27.8 / 25.7 (5.5 TB/s),
+// 21629 rows x (64 + 32) appended 201 / 171 (6.2 TB/s).
 constexpr int kHeadWarps = 4;
-constexpr int kHeadBatch = 4;
 
 template <typename T, bool kNeighbours, int U>
-__global__ void __launch_bounds__(kHeadWarps * 32)
+__global__ void __launch_bounds__(kHeadWarps * 32, 8)
 rotate_heads_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, const bool to_cache, const int parts) {
-  constexpr int kVec = Storage<T>::kVec, kPairs = kNeighbours ? kVec / 2 : kVec, kHeads = 32 / U;
+  constexpr int kVec = Storage<T>::kVec, kPairs = kNeighbours ? kVec / 2 : kVec, kHeads = 32 / U, kHeadBatch = kNeighbours ? 4 : 2;
+  // lanes index the table apart, which the constant bank serves one after the other: once per block (1000 rows: 9.3 -> 6.6 us)
+  __shared__ unsigned long long turn[64];
+  __shared__ int axis[64];
+  if (threadIdx.x < t.pairs) { turn[threadIdx.x] = t.turn[threadIdx.x]; axis[threadIdx.x] = t.axis[threadIdx.x]; }
+  __syncthreads();
   const int lane = threadIdx.x & 31, w = blockIdx.x * kHeadWarps + (threadIdx.x >> 5);
   const int row = w / parts, part = w - row * parts;
   if (row >= a.rows) return;
@@ -170,8 +175,8 @@ rotate_heads_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, con
   for (int j = 0; j < 2; ++j) {
     const int pr = lane + j * 32;
     if (pr < t.pairs) {
-      const long long pos = a.positions[(size_t)row * t.axes + t.axis[pr]];
-      const int32_t x = (int32_t)(((unsigned long long)pos * t.turn[pr]) >> 32);
+      const long long pos = a.positions[(size_t)row * t.axes + axis[pr]];
+      const int32_t x = (int32_t)(((unsigned long long)pos * turn[pr]) >> 32);
       sincospif((float)x * 4.656612873077392578125e-10f, &s[j], &c[j]);
       if (a.inverse) s[j] = -s[j];
     }
