@@ -592,6 +592,9 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
   a.cap = max_length < slots ? max_length : (int)slots;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   if (mode != D3TOM_WEIGHT_NONE) { a.scores = ctx->score_scratch; a.lse = ctx->lse_scratch; a.score_stride = ctx->vis_stride; }
+  // (a stride of whole 128-byte lines where the scratch allows)
+  if (mode != D3TOM_WEIGHT_NONE && ((a.cap + 31) & ~31) <= ctx->vis_stride) a.score_stride = (a.cap + 31) & ~31;
+  a.row_weight = row_weight; a.mass = ctx->score_scratch;
   a.part = ctx->attn_part_ws; a.joins = ctx->cached_joins;
   a.dev_status = ctx->dev_status;
   if (total_rows > 0) {
@@ -599,7 +602,7 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
     if (st != D3TOM_OK) return st;
   }
   if (mode != D3TOM_WEIGHT_NONE && a.cap > 0)
-    st = launch_cached_weight(ctx, a, cache->weight, mode == D3TOM_WEIGHT_ADD, row_weight, a.cap, s);
+    st = launch_cached_weight(ctx, a, cache->weight, mode == D3TOM_WEIGHT_ADD, tensor ? attn_cached_mass_columns(a) : 0, s);
   return st;
 }
 

@@ -63,8 +63,7 @@ constexpr int kWeightRows = 1024;      // rows x heads whose (M, f / l) are in s
 // Block (b, x): 128 slots of request b, four per lane; the warps share its rows x heads.
 template <int kWeightWarps>
 __global__ void __launch_bounds__(kWeightWarps * 32)
-weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, const float* __restrict__ row_weight,
-              const int chunks) {
+weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, const int chunks) {
   __shared__ float2 ml[kWeightRows];
   __shared__ float4 sum[kWeightWarps][32];
   grid_dependency_enter();
@@ -81,7 +80,7 @@ weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, con
     if (i0 > 0) __syncthreads();
     for (int i = threadIdx.x; i < many; i += kWeightWarps * 32) {
       const float2 x = a.lse[(size_t)r.lo * a.H + i0 + i];
-      const float f = row_weight != nullptr ? row_weight[r.lo + (i0 + i) / a.H] : 1.f;
+      const float f = a.row_weight != nullptr ? a.row_weight[r.lo + (i0 + i) / a.H] : 1.f;
       ml[i] = make_float2(-x.x, x.y == 0.f ? 0.f : f / x.y);
     }
     __syncthreads();
@@ -112,6 +111,24 @@ weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, con
   }
 }
 
+// Block (b, x): 128 slots of request b; adds up what the second pass over the keys left, one number for `columns` rows x heads.
+__global__ void __launch_bounds__(128)
+mass_kernel(const CachedArgs a, float* __restrict__ weight, const int add, const int chunks, const int columns) {
+  grid_dependency_enter();
+  const int b = blockIdx.x / chunks, slot = (blockIdx.x - b * chunks) * 128 + threadIdx.x;
+  const CachedRequest r = cached_request(a, b);
+  if (slot >= r.len) return;
+  float t = 0.f;
+  for (int f = 0; f < r.n * a.group; f += columns) {
+    const int i = f / a.group;
+    const float* row = a.mass + ((size_t)(r.lo + i) * a.H + (f - i * a.group)) * a.score_stride + slot;
+#pragma unroll 8
+    for (int g = 0; g < a.kv_heads; ++g) t += row[(size_t)g * a.group * a.score_stride];
+  }
+  const long long place = cached_place(a.page_table + (size_t)b * a.max_pages, slot, a.page_size, a.pages);
+  if (place >= 0) weight[place] = add ? weight[place] + t : t;
+}
+
 }  // namespace
 
 int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s) {
@@ -122,14 +139,14 @@ int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a,
   return D3TOM_OK;
 }
 
-int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, const float* row_weight,
-                         int max_length, cudaStream_t s) {
-  const int chunks = ceil_div(max_length, 128);
+int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, int mass_columns, cudaStream_t s) {
+  const int chunks = ceil_div(a.cap, 128);
   if ((long long)chunks * a.B > 0x7fffffffll) return D3TOM_ERR_UNSUPPORTED;
   // few rows: small blocks, many of them on an SM (64 requests of one row x 32 heads: 14 us with 8 warps, 30 with 16); many
   // rows: the loads of a block side by side (32 rows x 32 heads: 80 us with 8 warps one after the other, 21 with 16)
-  if ((long long)a.max_rows * a.H <= 256) D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<4>, chunks * a.B, 4 * 32, 0, s, a, weight, add, row_weight, chunks));
-  else D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<16>, chunks * a.B, 16 * 32, 0, s, a, weight, add, row_weight, chunks));
+  if (mass_columns > 0) D3TOM_CUDA_TRY(ctx, launch_serialized(mass_kernel, chunks * a.B, 128, 0, s, a, weight, add, chunks, mass_columns));
+  else if ((long long)a.max_rows * a.H <= 256) D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<4>, chunks * a.B, 4 * 32, 0, s, a, weight, add, chunks));
+  else D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<16>, chunks * a.B, 16 * 32, 0, s, a, weight, add, chunks));
   D3TOM_LAUNCH_CHECK(ctx);
   return D3TOM_OK;
 }

@@ -15,7 +15,12 @@
 // per lane until the segment ends.  Scores, maxima and sums are fp32; P is rounded to bf16 for the second product (2^-9 of
 // each term at most, unbiased), as in the other attention kernels.
 //
-//   warps 0 .. 3 (N = 128: 0 .. 7, a half of the columns each)  softmax and epilogue, a key / a number of O per thread
+// The mass per slot.  With few columns the raw scores go out (4 bytes per column, slot and key head, written and read again) and a
+// small kernel weighs them once M and l are known.  From some number of columns on that is more than the keys themselves: then the
+// same kernel runs a second time over the keys alone (kMass), takes the scores again, the same bits, and sums 2^(s c - M) f / l
+// over its columns, one number per slot and tile (launch_attn_cached_tc has the rule and what both take).
+//
+//   warps 0 .. 3 (or 0 .. 7, a half of the columns each)  softmax and epilogue, a key / a number of O per thread
 //   then one warp each: MMA issue, Q rows into shared memory, TMA producer of K, TMA producer of V
 // One CTA per SM walks its run of key tiles (cache_walk.cuh).  Every wait is bounded; after one that ran out the softmax
 // warps go through the rest of their run without waiting (their barriers need all of them), the other warps stop.
@@ -25,7 +30,9 @@
 namespace {
 
 template <int DH, int N> struct Shape {
-  static constexpr int kGroups = N > 64 ? 2 : 1;            // softmax warpgroups
+  // softmax warpgroups, each with its part of the columns (one / two, us: blocks of 32 rows x 32 heads x 128 68 / 65, of 64 rows 91 /
+  // 84; of 32 rows x 64, with two CTAs per SM instead, 49 / 52)
+  static constexpr int kGroups = N >= 64 || (N == 32 && DH == 128) ? 2 : 1;
   static constexpr int kCols = N / kGroups;                 // columns per softmax thread
   static constexpr int kSoftmaxWarps = 4 * kGroups;
   static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;
@@ -40,7 +47,7 @@ template <int DH, int N> struct Shape {
   static constexpr int kQBytes = N * DH * 2;
   static constexpr int kPBytes = N * kKeyTile * 2;
   static constexpr int kFloats = N * 7;                     // reference, factor, four warps' values, row numbers
-  static constexpr int kBars = 2 * kSlots + 2 * 2 + 2 + 2;
+  static constexpr int kBars = 2 * kSlots + 2 * 2 + 2 + 2 + 1;
   static constexpr int kBytes = 1024 + kSlots * kSlotBytes + kQBufs * kQBytes + kPBytes + kFloats * 4 + kBars * 8 + 64;
   static_assert(kPerSm * (kBytes + 1024) <= 228 * 1024, "shared memory of an SM");
   static constexpr uint32_t kTmemCols = N == 16 ? 64 : 4 * N;   // S twice and O: 3 N, as a power of two
@@ -62,7 +69,7 @@ __device__ __forceinline__ float lane_sums(float (&v)[C]) {
   return v[0];
 }
 
-template <int DH, int N>
+template <int DH, int N, bool kMass>
 __global__ void __launch_bounds__(Shape<DH, N>::kThreads, Shape<DH, N>::kPerSm)
 attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const CachedArgs a,
                       const int box) {
@@ -84,8 +91,8 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
   uint64_t* q_full = kv_empty + kSlots;                 // [2]
   uint64_t* q_empty = q_full + 2;                       // [2]
   uint64_t* s_full = q_empty + 2;                       // [2]
-  uint64_t* p_full = s_full + 2;
-  uint64_t* pv_done = p_full + 1;
+  uint64_t* p_full = s_full + 2;                        // [2] (kMass: a tile's scores have been read; otherwise the first alone, P written)
+  uint64_t* pv_done = p_full + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(pv_done + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile uint32_t* bad_boxes = tmem_slot + 2;         // [8] per key tile: boxes whose page is not one of the pool's
@@ -94,7 +101,7 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) { ptx::mbar_init(&kv_full[i], 1); ptx::mbar_init(&kv_empty[i], 1); }
     for (int i = 0; i < 2; ++i) { ptx::mbar_init(&q_full[i], 1); ptx::mbar_init(&q_empty[i], 1); ptx::mbar_init(&s_full[i], 1); }
-    ptx::mbar_init(p_full, S::kSoftmaxWarps);
+    for (int i = 0; i < 2; ++i) ptx::mbar_init(&p_full[i], S::kSoftmaxWarps);
     ptx::mbar_init(pv_done, 1);
     *abort_flag = 0;
     ptx::fence_mbar_init();
@@ -113,16 +120,16 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
 
   if (warp >= S::kSoftmaxWarps + 2) {
     // ------------------------------------------------------------ TMA producers, one for K and one for V: a lane per page part
-    const int kind = warp - (S::kSoftmaxWarps + 2);
+    const int kind = warp - (S::kSoftmaxWarps + 2);     // (kMass: nobody wants V)
     const CUtensorMap* tmap = kind == 0 ? &tmap_k : &tmap_v;
     if (lane == 0) ptx::prefetch_tensormap(tmap);
     const int boxes = kKeyTile / box, outside = a.pages * a.page_size;
-    // a cache that is read once need not push the scores out of L2
-    const uint64_t policy = ptx::l2_policy(a.read_once != 0);
+    // what is read once need not push the scores, or the keys that a second pass wants, out of L2
+    const uint64_t policy = ptx::l2_policy(kind == 0 ? a.read_once != 0 && !a.keys_again : a.read_once != 0);
     int ring = kind, issued = 0, tile = 0;
     uint32_t phase = 1;                                 // of the ring's `empty` barriers: the first round finds them so
     bool ok = true;
-    while (ok && walk.next(a, s)) {
+    while (ok && (!kMass || kind == 0) && walk.next(a, s)) {
       const int32_t* table = a.page_table + (size_t)s.b * a.max_pages;
       auto find = [&](int t) -> int {                   // row of this lane's box in the pool; behind its end: nothing, zeros
         const int slot = t * kKeyTile + lane * box;
@@ -130,11 +137,13 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         const long long at = cached_place(table, slot, a.page_size, a.pages);
         return at < 0 ? -1 : (int)at;
       };
-      int row = find(s.t0);
+      // the second pass goes through a segment backwards: what the first one read last is still in L2
+      auto at = [&](int t) { return kMass ? s.t0 + s.t1 - 1 - t : t; };
+      int row = find(at(s.t0));
       for (int t = s.t0; t < s.t1; ++t, ++tile) {
         const uint32_t bad = __ballot_sync(0xffffffffu, row < 0);
         if (row < 0) { row = outside; atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG); }
-        const int next_row = t + 1 < s.t1 ? find(t + 1) : outside;
+        const int next_row = t + 1 < s.t1 ? find(at(t + 1)) : outside;
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&kv_empty[ring], phase, abort_flag, a.dev_status));
         if (!ok) break;
         if (lane == 0 && kind == 0) bad_boxes[tile & 7] = bad;   // (at most seven tiles ahead of the softmax warps)
@@ -173,6 +182,10 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       bool ok = true, v_first = false;
       auto advance = [&](int& ring, uint32_t& phase) { ring += 2; if (ring >= kSlots) { ring -= kSlots; phase ^= 1u; } };
       auto issue_pv = [&](int t) {                      // of tile t, whose V is at v_ring
+        if constexpr (kMass) {                          // (its scores have been read, that is all)
+          ok = ptx::mbar_wait(&p_full[t & 1], (uint32_t)(t >> 1) & 1u, abort_flag, a.dev_status);
+          return;
+        }
         ok = ptx::mbar_wait(&kv_full[v_ring], v_phase, abort_flag, a.dev_status) &&
              ptx::mbar_wait(p_full, (uint32_t)t & 1u, abort_flag, a.dev_status);
         if (!ok) return;
@@ -240,8 +253,10 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&q_full[qb]);
     }
-    if (lane == 0) cached_write_join(a, run, blockIdx.x, head, head_tiles);
-    cached_write_empty<__nv_bfloat16>(a, lane, 32);
+    if constexpr (!kMass) {
+      if (lane == 0) cached_write_join(a, run, blockIdx.x, head, head_tiles);
+      cached_write_empty<__nv_bfloat16>(a, lane, 32);
+    }
   } else {
     // ------------------------------------------------------------ softmax and epilogue
     const int quarter = warp & 3, group = warp >> 2, col0 = group * kCols;
@@ -266,7 +281,42 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
 #pragma unroll
         for (int i = 0; i < kCols; ++i) e[i] = -INFINITY;
     };
-    while (walk.next(a, s)) {
+    if constexpr (kMass) {
+      while (walk.next(a, s)) {
+        ptx::named_sync(bar, 128);                      // (the last segment's columns are done with)
+        const int cols = min(kCols, s.rows - col0);
+        if (gt < kCols) {
+          float m = 0.f, f = 0.f;
+          if (gt < cols) {
+            const int row = cached_row_index(a, s, col0 + gt);
+            const float2 ml = a.lse[row];
+            m = -ml.x;
+            f = ml.y == 0.f ? 0.f : (a.row_weight != nullptr ? a.row_weight[row / a.H] : 1.f) / ml.y;
+          }
+          negm_s[col0 + gt] = m;
+          alpha_s[col0 + gt] = f;
+        }
+        ptx::named_sync(bar, 128);
+        float* mass = cols > 0 ? a.mass + (size_t)cached_row_index(a, s, col0) * a.score_stride : nullptr;
+        for (int t = s.t1 - 1; t >= s.t0; --t, ++tile) {
+          const int slot = t * kKeyTile + key;
+          ptx::mbar_wait(&s_full[tile & 1], (uint32_t)(tile >> 1) & 1u, abort_flag, a.dev_status);
+          ptx::tc_fence_after_sync();
+          load_scores(tile & 1, true);
+          ptx::tc_fence_before_sync();
+          __syncwarp();
+          // two barriers: nothing holds a warp back from the next tile's scores, which are there, before the others have read
+          // these; the tile after that one waits for all of them
+          if (lane == 0) ptx::mbar_arrive(&p_full[tile & 1]);
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < kCols; ++i)
+            if (i < cols) sum += alpha_s[col0 + i] * ptx::ex2(fmaf(e[i], c, negm_s[col0 + i]));
+          if (mass != nullptr && slot < s.len) mass[slot] = sum;
+        }
+      }
+    }
+    while (!kMass && walk.next(a, s)) {
       // (the barrier at the end of the last segment lies behind every use of row_s)
       if (gt < kCols) row_s[col0 + gt] = col0 + gt < s.rows ? cached_row_index(a, s, col0 + gt) : -1;
       const int cols = min(kCols, s.rows - col0);       // columns in use (none or less: padding only)
@@ -412,39 +462,63 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
   if (warp == 0) ptx::tmem_dealloc(tmem, S::kTmemCols);
 }
 
-template <int DH, int N>
-int launch(d3tom_ctx* ctx, CachedArgs a, cudaStream_t s) {
-  using Sh = Shape<DH, N>;
-  int box = kKeyTile;                                   // rows per copy: a power of two that divides the page
-  while (a.page_size % box != 0) box >>= 1;
-  CUtensorMap tk, tv;
-  const uint64_t rows = (uint64_t)a.pages * a.page_size, cols = (uint64_t)a.kv_heads * DH;
-  int r = make_tmap_bf16_2d(&tk, a.k, rows, cols, cols, (uint32_t)box, 64, DH == 64);
-  if (r == 0) r = make_tmap_bf16_2d(&tv, a.v, rows, cols, cols, (uint32_t)box, 64, DH == 64);
+// What a launch takes apart from the arguments: the tensor maps and the rows per copy.
+struct CacheMaps { CUtensorMap k, v; int box; };
+int make_maps(d3tom_ctx* ctx, const CachedArgs& a, CacheMaps* m) {
+  m->box = kKeyTile;                                    // rows per copy: a power of two that divides the page
+  while (a.page_size % m->box != 0) m->box >>= 1;
+  const uint64_t rows = (uint64_t)a.pages * a.page_size, cols = (uint64_t)a.kv_heads * a.dh;
+  int r = make_tmap_bf16_2d(&m->k, a.k, rows, cols, cols, (uint32_t)m->box, 64, a.dh == 64);
+  if (r == 0) r = make_tmap_bf16_2d(&m->v, a.v, rows, cols, cols, (uint32_t)m->box, 64, a.dh == 64);
   if (r != 0) { ctx->last_cuda_error = r; return D3TOM_ERR_CUDA; }
+  return D3TOM_OK;
+}
+
+template <int DH, int N>
+int launch(d3tom_ctx* ctx, CachedArgs a, bool mass, cudaStream_t s) {
+  using Sh = Shape<DH, N>;
+  CacheMaps m;
+  const int st = make_maps(ctx, a, &m);
+  if (st != D3TOM_OK) return st;
   a.tile_rows = N;
   a.read_once = (long long)a.max_rows * a.group <= N;
+  a.keys_again = mass;
   a.ctas = Sh::kPerSm * ctx->sm_count;
-  auto kernel = attn_cached_tc_kernel<DH, N>;
+  if (mass) a.scores = nullptr;
+  auto kernel = attn_cached_tc_kernel<DH, N, false>;
   D3TOM_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes));
-  D3TOM_CUDA_TRY(ctx, launch_serialized(kernel, a.ctas, Sh::kThreads, Sh::kBytes, s, tk, tv, a, box));
+  D3TOM_CUDA_TRY(ctx, launch_serialized(kernel, a.ctas, Sh::kThreads, Sh::kBytes, s, m.k, m.v, a, m.box));
   D3TOM_LAUNCH_CHECK(ctx);
-  return launch_attn_cached_join(ctx, D3TOM_BF16, a, s);
+  const int joined = launch_attn_cached_join(ctx, D3TOM_BF16, a, s);
+  if (joined != D3TOM_OK || !mass) return joined;
+  auto again = attn_cached_tc_kernel<DH, N, true>;
+  D3TOM_CUDA_TRY(ctx, cudaFuncSetAttribute(again, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes));
+  D3TOM_CUDA_TRY(ctx, launch_serialized(again, a.ctas, Sh::kThreads, Sh::kBytes, s, m.k, m.v, a, m.box));
+  D3TOM_LAUNCH_CHECK(ctx);
+  return D3TOM_OK;
 }
 
 template <int DH>
-int launch_columns(d3tom_ctx* ctx, const CachedArgs& a, cudaStream_t s) {
+int launch_columns(d3tom_ctx* ctx, const CachedArgs& a, bool mass, cudaStream_t s) {
   const long long rows = (long long)a.max_rows * a.group;
-  if (rows <= 16) return launch<DH, 16>(ctx, a, s);
-  if (rows <= 32) return launch<DH, 32>(ctx, a, s);
-  if (rows <= 64) return launch<DH, 64>(ctx, a, s);
-  return launch<DH, 128>(ctx, a, s);
+  if (rows <= 16) return launch<DH, 16>(ctx, a, mass, s);
+  if (rows <= 32) return launch<DH, 32>(ctx, a, mass, s);
+  if (rows <= 64) return launch<DH, 64>(ctx, a, mass, s);
+  return launch<DH, 128>(ctx, a, mass, s);
 }
 
 }  // namespace
 
+// Whether the mass per slot comes from a second pass over the keys; the columns whose sums are then one number, 0 if not.
+int attn_cached_mass_columns(const CachedArgs& a) {
+  const long long rows = (long long)a.max_rows * a.group;
+  if (rows * 3 <= a.dh) return 0;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
+
 int launch_attn_cached_tc(d3tom_ctx* ctx, const CachedArgs& a, cudaStream_t s) {
-  if (a.dh == 128) return launch_columns<128>(ctx, a, s);
-  if (a.dh == 64) return launch_columns<64>(ctx, a, s);
+  const bool mass = a.scores != nullptr && attn_cached_mass_columns(a) > 0;
+  if (a.dh == 128) return launch_columns<128>(ctx, a, mass, s);
+  if (a.dh == 64) return launch_columns<64>(ctx, a, mass, s);
   return D3TOM_ERR_UNSUPPORTED;
 }

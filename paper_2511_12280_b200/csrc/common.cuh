@@ -242,15 +242,16 @@ struct CachedArgs {
   int pages, page_size, max_pages, cap;   // cap: slots a request can have in this call
   float scale_log2;             // softmax_scale * log2(e)
   float* scores; float2* lse; int score_stride;   // [total_rows][H][score_stride] raw q.k and [total_rows][H] (M, l); null without weights
+  const float* row_weight; float* mass;     // second pass over the keys: [total_rows] or null; sums, at the scores' place
   float* part;                  // [ctas][2] parts of work items that several CTAs share (cache_walk.cuh)
   int* joins;                   // [ctas][8] what the join has to do
-  int tile_rows, ctas, read_once;   // set by the launcher; read_once: no item shares its keys with another
+  int tile_rows, ctas, read_once, keys_again;   // set by the launcher; read_once: no item shares its keys with another
   int* dev_status;
 };
 int launch_attn_cached_simt(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
 int launch_attn_cached_tc(d3tom_ctx* ctx, const CachedArgs& a, cudaStream_t s);
 int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);
-int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, const float* row_weight,
-                         int max_length, cudaStream_t s);
+int attn_cached_mass_columns(const CachedArgs& a);   // 0: the scores went out
+int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, int mass_columns, cudaStream_t s);
 int launch_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache& cache, const int32_t* budget,
                        const int32_t* protect_from, int B, int max_length, int32_t* length_out, cudaStream_t s);
