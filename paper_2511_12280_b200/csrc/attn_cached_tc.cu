@@ -124,8 +124,9 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     const CUtensorMap* tmap = kind == 0 ? &tmap_k : &tmap_v;
     if (lane == 0) ptx::prefetch_tensormap(tmap);
     const int boxes = kKeyTile / box, outside = a.pages * a.page_size;
-    // what is read once need not push the scores, or the keys that a second pass wants, out of L2
-    const uint64_t policy = ptx::l2_policy(kind == 0 ? a.read_once != 0 && !a.keys_again : a.read_once != 0);
+    // what is read once need not push the scores out of L2.  (Keeping the keys there for a second pass cost more than it gave:
+    // 32 rows x 32 heads 110 -> 119 us.)
+    const uint64_t policy = ptx::l2_policy(a.read_once != 0);
     int ring = kind, issued = 0, tile = 0;
     uint32_t phase = 1;                                 // of the ring's `empty` barriers: the first round finds them so
     bool ok = true;
@@ -137,13 +138,11 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         const long long at = cached_place(table, slot, a.page_size, a.pages);
         return at < 0 ? -1 : (int)at;
       };
-      // the second pass goes through a segment backwards: what the first one read last is still in L2
-      auto at = [&](int t) { return kMass ? s.t0 + s.t1 - 1 - t : t; };
-      int row = find(at(s.t0));
+      int row = find(s.t0);
       for (int t = s.t0; t < s.t1; ++t, ++tile) {
         const uint32_t bad = __ballot_sync(0xffffffffu, row < 0);
         if (row < 0) { row = outside; atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG); }
-        const int next_row = t + 1 < s.t1 ? find(at(t + 1)) : outside;
+        const int next_row = t + 1 < s.t1 ? find(t + 1) : outside;
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&kv_empty[ring], phase, abort_flag, a.dev_status));
         if (!ok) break;
         if (lane == 0 && kind == 0) bad_boxes[tile & 7] = bad;   // (at most seven tiles ahead of the softmax warps)
@@ -298,7 +297,7 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         }
         ptx::named_sync(bar, 128);
         float* mass = cols > 0 ? a.mass + (size_t)cached_row_index(a, s, col0) * a.score_stride : nullptr;
-        for (int t = s.t1 - 1; t >= s.t0; --t, ++tile) {
+        for (int t = s.t0; t < s.t1; ++t, ++tile) {
           const int slot = t * kKeyTile + key;
           ptx::mbar_wait(&s_full[tile & 1], (uint32_t)(tile >> 1) & 1u, abort_flag, a.dev_status);
           ptx::tc_fence_after_sync();
@@ -482,7 +481,6 @@ int launch(d3tom_ctx* ctx, CachedArgs a, bool mass, cudaStream_t s) {
   if (st != D3TOM_OK) return st;
   a.tile_rows = N;
   a.read_once = (long long)a.max_rows * a.group <= N;
-  a.keys_again = mass;
   a.ctas = Sh::kPerSm * ctx->sm_count;
   if (mass) a.scores = nullptr;
   auto kernel = attn_cached_tc_kernel<DH, N, false>;
@@ -491,10 +489,12 @@ int launch(d3tom_ctx* ctx, CachedArgs a, bool mass, cudaStream_t s) {
   D3TOM_LAUNCH_CHECK(ctx);
   const int joined = launch_attn_cached_join(ctx, D3TOM_BF16, a, s);
   if (joined != D3TOM_OK || !mass) return joined;
-  auto again = attn_cached_tc_kernel<DH, N, true>;
-  D3TOM_CUDA_TRY(ctx, cudaFuncSetAttribute(again, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes));
-  D3TOM_CUDA_TRY(ctx, launch_serialized(again, a.ctas, Sh::kThreads, Sh::kBytes, s, m.k, m.v, a, m.box));
-  D3TOM_LAUNCH_CHECK(ctx);
+  if constexpr (N > 16) {                               // (so few columns never ask for a second pass)
+    auto again = attn_cached_tc_kernel<DH, N, true>;
+    D3TOM_CUDA_TRY(ctx, cudaFuncSetAttribute(again, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::kBytes));
+    D3TOM_CUDA_TRY(ctx, launch_serialized(again, a.ctas, Sh::kThreads, Sh::kBytes, s, m.k, m.v, a, m.box));
+    D3TOM_LAUNCH_CHECK(ctx);
+  }
   return D3TOM_OK;
 }
 
@@ -510,10 +510,14 @@ int launch_columns(d3tom_ctx* ctx, const CachedArgs& a, bool mass, cudaStream_t 
 }  // namespace
 
 // Whether the mass per slot comes from a second pass over the keys; the columns whose sums are then one number, 0 if not.
+// Per slot and key head the scores are 8 bytes a column, written and read, the keys 2 dh bytes and a pass has its own ramp.  us, scores
+// out / second pass, eight requests of up to 4288 slots: 32 heads x 128, 16 rows 83 / 103, 32 113 / 114, 64 164 / 138; 32 x 64, 16 rows
+// 59 / 63, 24 80 / 74, 32 94 / 77; 32 heads on 8 x 128, 16 rows (64 columns) 56 / 61, 32 (128) 144 / 100.
 int attn_cached_mass_columns(const CachedArgs& a) {
   const long long rows = (long long)a.max_rows * a.group;
-  if (rows * 3 <= a.dh) return 0;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  if (8 * rows < 64 + 2 * a.dh) return 0;
+  if (a.dh == 128) return rows <= 32 ? Shape<128, 32>::kCols : rows <= 64 ? Shape<128, 64>::kCols : Shape<128, 128>::kCols;
+  return rows <= 32 ? Shape<64, 32>::kCols : rows <= 64 ? Shape<64, 64>::kCols : Shape<64, 128>::kCols;
 }
 
 int launch_attn_cached_tc(d3tom_ctx* ctx, const CachedArgs& a, cudaStream_t s) {

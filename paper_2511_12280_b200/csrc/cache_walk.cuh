@@ -63,6 +63,16 @@ __device__ __forceinline__ CachedRun cached_run(const CachedArgs& a, int cta) {
   CachedRun run;
   run.total = total;
   run.ctas = total < a.ctas ? (int)total : a.ctas;
+  if (a.B == 1 && total > a.ctas) {
+    // one request: as many CTAs as its items share evenly, if that is at most a tile more for each; none then ends one item and
+    // begins another, which costs it a second first tile and a second result
+    const CachedRequest r = cached_request(a, 0);
+    const int items = a.kv_heads * cached_row_tiles(a, r.n);
+    if (items <= a.ctas) {
+      const int even = a.ctas / items * items;
+      if (total * (a.ctas - even) <= (long long)a.ctas * even) run.ctas = even;
+    }
+  }
   run.b = 0; run.base = 0; run.w0 = run.w1 = total;
   if (cta >= run.ctas) return run;
   run.w0 = cached_run_begin(total, run.ctas, cta);

@@ -245,7 +245,7 @@ struct CachedArgs {
   const float* row_weight; float* mass;     // second pass over the keys: [total_rows] or null; sums, at the scores' place
   float* part;                  // [ctas][2] parts of work items that several CTAs share (cache_walk.cuh)
   int* joins;                   // [ctas][8] what the join has to do
-  int tile_rows, ctas, read_once, keys_again;   // set by the launcher; read_once: no item shares its keys with another
+  int tile_rows, ctas, read_once;   // set by the launcher; read_once: no item shares its keys with another
   int* dev_status;
 };
 int launch_attn_cached_simt(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s);

@@ -318,6 +318,43 @@ def test_attention_without_rows_or_slots(dt):
 
 
 @pytest.mark.parametrize("dt", [BF, FP])
+def test_attention_of_no_rows_at_all(dt):
+    P = Pool([300, 20], 8, 2, 64, dt, seed=12)
+    q = randn((1, 4, 64), dt, 1)
+    out = torch.full((1, 256), 3.0, dtype=dt, device=DEV)
+    ctx = B_.Context(4, 2, 4, 64, 4, 300)
+    before = P.copy()[2]
+    for mode, want in ((B_.WEIGHT_NONE, None), (B_.WEIGHT_ADD, None), (B_.WEIGHT_SET, 0.0)):
+        ctx.d3tom_attn_cached(P.cache, q, i32([0, 0, 0]), 2, 0, 0, 300, 0.125, mode, None, out)
+        for b in range(2):
+            at = torch.as_tensor(P.at[b], device=DEV)
+            assert torch.equal(P.flat()[2][at], before[at] if want is None else torch.zeros_like(before[at]))
+    assert (out == 3).all() and ctx.device_status() == 0
+
+
+@pytest.mark.parametrize("block,H,kv", [(32, 2, 2), (70, 4, 1), (9, 8, 2)])
+def test_weights_leave_out_a_page_that_is_not_there(block, H, kv):
+    # the same with so many rows that the weights come from a second pass over the keys
+    P = Pool([700], 16, kv, 128, BF, seed=23)
+    P.table[0, 3] = P.pages
+    whole = P.at[0]
+    there = np.concatenate([whole[:48], whole[64:]])
+    q = randn((block, H, 128), BF, 1)
+    out = torch.zeros(block, H * 128, dtype=BF, device=DEV)
+    ctx = B_.Context(block, 1, H, 128, block, 700)
+    ctx.d3tom_attn_cached(P.cache, q, i32([0, block]), 1, block, block, 700, 128 ** -0.5, B_.WEIGHT_SET, None, out)
+    assert ctx.device_status() == B_.ERR_INVALID_ARG
+    k1, v1, w1, _ = P.flat()
+    idx = torch.as_tensor(there, device=DEV)
+    o, p, mag, _ = co.attend(f64(q), f64(k1[idx]), f64(v1[idx]), 128 ** -0.5)
+    assert (np.abs(f64(out).reshape(o.shape) - o) <= 2.0 ** -7 * mag + 1e-4).all()
+    mass = p.sum(axis=(0, 1))
+    assert (np.abs(f64(w1)[there] - mass) <= 1e-3 * mass).all()
+    gone = torch.as_tensor(whole[48:64], device=DEV)
+    assert torch.equal(w1[gone], P.copy()[2][gone]) and torch.isfinite(w1[gone]).all()
+
+
+@pytest.mark.parametrize("dt", [BF, FP])
 def test_attention_leaves_out_what_is_not_there(dt):
     # a page that is not in the pool, and a length beyond the table: as if those slots were not there
     P = Pool([300, 64], 16, 1, 64, dt, seed=13)
