@@ -393,7 +393,7 @@ int d3tom_attn_cached(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, 
  *  protect_from  [B] int32 or NULL (no slot is protected); needs cache->token
  *  length_out    [B] int32; may be the array cache->length
  *  max_length    host: >= every length[b]
- * No two requests of a call may share a page that is moved into.  Scratch: B * (max_length + 3) words out of
+ * No two requests of a call may share a page that is moved into.  Scratch: B * (max_length + 1) words out of
  * max_total_tokens * heads * dh, D3TOM_ERR_WORKSPACE beyond. */
 int d3tom_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const int32_t* budget,
                       const int32_t* protect_from, int B, int max_length, int32_t* length_out, d3tom_stream stream);

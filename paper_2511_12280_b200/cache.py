@@ -4,7 +4,8 @@
 
 ``PagedCache`` owns the pools, hands out pages and keeps the host's copy of the lengths (all sizes are known on the host, as
 everywhere in this package); every step of the path runs in the library's kernels.  Slots of a request are in no order that
-matters to attention; ``token`` holds the number that the caller gave a slot's token.
+matters to attention; ``token`` holds the number that the caller gave a slot's token.  All work, the small uploads of table
+and lengths included, is enqueued on torch's current stream.
 """
 from __future__ import annotations
 
@@ -25,7 +26,7 @@ class PagedCache:
         self.batch, self.heads, self.kv_heads, self.dh, self.dtype = batch, heads, kv_heads, head_dim, dtype
         self.page_size, self.max_length = page_size, max_length
         # the scratch of an eviction is counted in words of max_total_tokens rows
-        tokens = max(max_rows, -(-batch * (max_length + 3) // (heads * head_dim)))
+        tokens = max(max_rows, -(-batch * (max_length + 1) // (heads * head_dim)))
         self.ctx = B_.Context(tokens, batch, heads, head_dim, max(1, max_scored_rows), max(1, max_length), device)
         shape = (pages, page_size)
         kw = dict(device=self.dev)
@@ -63,24 +64,24 @@ class PagedCache:
         return torch.as_tensor(np.concatenate([[0], np.cumsum(rows)]).astype(np.int32), device=self.dev)
 
     def append(self, rows: Sequence[int], k, v, tokens, q=None, q_out=None, spec: Optional[B_.RopeSpec] = None,
-               positions=None, first_weight=None, stream=None):
+               positions=None, first_weight=None):
         """Writes rows[b] new rows of every request behind its slots; q rotated alike goes to q_out.  first_weight +inf
         keeps a row from being evicted."""
         if len(rows) != self.batch:
             raise ValueError("rows of every request")
         self._resize([n + r for n, r in zip(self.lengths_h, rows)])
         self.ctx.d3tom_cache_append(self.cache, spec, q, k, v, positions, tokens, first_weight, self._cu(rows), self.batch,
-                                    int(sum(rows)), q_out, stream)
+                                    int(sum(rows)), q_out)
 
-    def attend(self, rows: Sequence[int], q, out, mode: int = B_.WEIGHT_NONE, row_weight=None, stream=None):
+    def attend(self, rows: Sequence[int], q, out, mode: int = B_.WEIGHT_NONE, row_weight=None):
         """Attention of rows[b] rows of every request over all of its slots."""
         self.ctx.d3tom_attn_cached(self.cache, q, self._cu(rows), self.batch, int(sum(rows)), max(rows), max(self.lengths_h),
-                                   self.scale, mode, row_weight, out, stream)
+                                   self.scale, mode, row_weight, out)
 
-    def evict(self, budget: Sequence[int], protect_from=None, stream=None):
+    def evict(self, budget: Sequence[int], protect_from=None):
         """Keeps the min(budget[b], length) heaviest slots of every request; frees the pages behind them."""
         want = torch.as_tensor(np.asarray(budget, dtype=np.int32), device=self.dev)
-        self.ctx.d3tom_cache_evict(self.cache, want, protect_from, self.batch, max(self.lengths_h), self.length, stream)
+        self.ctx.d3tom_cache_evict(self.cache, want, protect_from, self.batch, max(self.lengths_h), self.length)
         self._resize([min(max(int(x), 0), n) for x, n in zip(budget, self.lengths_h)])
 
     def drop_last(self, rows: Sequence[int]):

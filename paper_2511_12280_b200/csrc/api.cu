@@ -592,8 +592,6 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
   a.cap = max_length < slots ? max_length : (int)slots;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   if (mode != D3TOM_WEIGHT_NONE) { a.scores = ctx->score_scratch; a.lse = ctx->lse_scratch; a.score_stride = ctx->vis_stride; }
-  // (a stride of whole 128-byte lines where the scratch allows)
-  if (mode != D3TOM_WEIGHT_NONE && ((a.cap + 31) & ~31) <= ctx->vis_stride) a.score_stride = (a.cap + 31) & ~31;
   a.row_weight = row_weight; a.mass = ctx->score_scratch;
   a.part = ctx->attn_part_ws; a.joins = ctx->cached_joins;
   a.dev_status = ctx->dev_status;
@@ -624,7 +622,7 @@ static int evict_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, 
     return D3TOM_ERR_INVALID_ARG;
   const int row_bytes = ctx->lim.head_dim * (dt == D3TOM_BF16 ? 2 : 4);
   if (row_bytes % 8 != 0) return D3TOM_ERR_UNSUPPORTED;
-  if ((long long)B * ((long long)max_length + 3) > (long long)ctx->lim.max_total_tokens * ctx->lim.heads * ctx->lim.head_dim)
+  if ((long long)B * ((long long)max_length + 1) > (long long)ctx->lim.max_total_tokens * ctx->lim.heads * ctx->lim.head_dim)
     return D3TOM_ERR_WORKSPACE;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return D3TOM_ERR_CUDA;

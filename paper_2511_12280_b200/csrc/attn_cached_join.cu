@@ -74,22 +74,24 @@ weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, con
   if (first >= r.len) return;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   const int rows = r.n * a.H;
-  const bool has = slot0 < r.len;               // (the stride is a multiple of four: a float4 ends inside it)
+  const bool has = slot0 < r.len;               // (the pitch is a multiple of four: a float4 ends inside it)
+  const CachedScores scores = cached_scores(a, r.lo, r.n, r.len, first / kKeyTile);
   for (int i0 = 0; i0 < rows; i0 += kWeightRows) {
     const int many = min(kWeightRows, rows - i0);
     if (i0 > 0) __syncthreads();
     for (int i = threadIdx.x; i < many; i += kWeightWarps * 32) {
-      const float2 x = a.lse[(size_t)r.lo * a.H + i0 + i];
-      const float f = a.row_weight != nullptr ? a.row_weight[r.lo + (i0 + i) / a.H] : 1.f;
+      const int per_head = r.n * a.group, g = (i0 + i) / per_head, in = i0 + i - g * per_head, row = r.lo + in / a.group;   // (cached_scores)
+      const float2 x = a.lse[(size_t)row * a.H + g * a.group + in % a.group];
+      const float f = a.row_weight != nullptr ? a.row_weight[row] : 1.f;
       ml[i] = make_float2(-x.x, x.y == 0.f ? 0.f : f / x.y);
     }
     __syncthreads();
     if (has) {
-      const float* sc = a.scores + ((size_t)r.lo * a.H + i0) * a.score_stride + slot0;
+      const float* sc = scores.tile + (size_t)i0 * scores.pitch + lane * 4;
 #pragma unroll 8
       for (int i = warp; i < many; i += kWeightWarps) {
         const float2 f = ml[i];
-        const float4 s = __ldcs(reinterpret_cast<const float4*>(sc + (size_t)i * a.score_stride));
+        const float4 s = __ldcs(reinterpret_cast<const float4*>(sc + (size_t)i * scores.pitch));
         acc.x += f.y * ptx::ex2(fmaf(s.x, a.scale_log2, f.x));
         acc.y += f.y * ptx::ex2(fmaf(s.y, a.scale_log2, f.x));
         acc.z += f.y * ptx::ex2(fmaf(s.z, a.scale_log2, f.x));

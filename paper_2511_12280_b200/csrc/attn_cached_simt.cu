@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
       if (r < s.rows && has) q[r] = load4(static_cast<const T*>(a.q) + (size_t)cached_row_index(a, s, r) * dh + d0);
     }
     const int my_row = lane % RT;
-    float* score_row = a.scores != nullptr && my_row < s.rows ? a.scores + (size_t)cached_row_index(a, s, my_row) * a.score_stride : nullptr;
+    const bool scored = a.scores != nullptr && my_row < s.rows;
     float m = -INFINITY, l = 0.f;                // of this lane's row, over its own pairs (l) and all lanes' (m)
     const int end = min(s.len, s.t1 * kKeyTile);
     for (int key0 = s.t0 * kKeyTile + warp * kKeys; key0 < end; key0 += kWarps * kKeys) {
@@ -98,7 +98,11 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
       }
       const int key = sub / RT * kSide + side, mine = __shfl_sync(0xffffffffu, at, key);
       const float raw = val[0];
-      if (score_row != nullptr && mine >= 0) score_row[key0 + key] = raw;
+      if (scored && mine >= 0) {
+        const int t = (key0 + key) / kKeyTile;
+        const CachedScores sc = cached_scores(a, s.lo, s.n, s.len, t);
+        sc.tile[(size_t)(s.kv_head * s.n * a.group + s.row0 + my_row) * sc.pitch + (key0 + key - t * kKeyTile)] = raw;
+      }
       const float x = mine >= 0 ? raw * a.scale_log2 : -INFINITY;
       float top = x;
 #pragma unroll

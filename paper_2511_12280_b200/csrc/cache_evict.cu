@@ -21,7 +21,7 @@ struct EvictArgs {
   d3tom_cache cache;
   const int32_t* budget; const int32_t* protect_from; int32_t* length_out;
   int B, cap;                   // cap: slots a request can have in this call
-  int32_t* gaps; int32_t* movers;     // [B][cap / 2 + 1] places in the pools; the movers last first
+  int32_t* gaps; int32_t* movers;     // [B][max_length / 2] places in the pools; the movers last first
   int32_t* count;               // [B] moves
   int list_stride;
   int* dev_status;
@@ -341,8 +341,8 @@ int launch_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache& cache,
   const long long slots = (long long)cache.max_pages * cache.page_size;
   a.cache = cache; a.budget = budget; a.protect_from = protect_from; a.length_out = length_out; a.B = B;
   a.cap = max_length < slots ? max_length : (int)slots;
-  a.list_stride = max_length / 2 + 1;            // moves are at most min(keep, n - keep)
-  a.count = static_cast<int32_t*>(ctx->kept_rows);     // (B + 2 B (max_length / 2 + 1) words at most)
+  a.list_stride = max_length / 2;                // moves are at most min(keep, n - keep)
+  a.count = static_cast<int32_t*>(ctx->kept_rows);     // (B + 2 B (max_length / 2) words)
   a.gaps = a.count + B;
   a.movers = a.gaps + (size_t)B * a.list_stride;
   a.dev_status = ctx->dev_status;
@@ -351,7 +351,7 @@ int launch_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache& cache,
   D3TOM_CUDA_TRY(ctx, launch_serialized(plan, B, kThreads, 0, s, a));
   const int row_bytes = cache.kv_heads * ctx->lim.head_dim * (dt == D3TOM_BF16 ? 2 : 4);
   const long long most = (long long)B * a.list_stride;
-  const int blocks = most < 8 * ctx->sm_count ? (int)most : 8 * ctx->sm_count;
+  const int blocks = most < 1 ? 1 : most < 8 * ctx->sm_count ? (int)most : 8 * ctx->sm_count;
   if (row_bytes % 16 == 0) D3TOM_CUDA_TRY(ctx, launch_serialized(move_kernel<uint4>, blocks, kMoveThreads, 0, s, a, row_bytes / 16));
   else D3TOM_CUDA_TRY(ctx, launch_serialized(move_kernel<uint2>, blocks, kMoveThreads, 0, s, a, row_bytes / 8));
   D3TOM_LAUNCH_CHECK(ctx);

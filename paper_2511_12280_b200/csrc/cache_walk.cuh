@@ -96,7 +96,7 @@ __device__ __forceinline__ CachedRun cached_run(const CachedArgs& a, int cta) {
 
 // The segments of a run, one after the other.
 struct CachedSegment {
-  int b, len, lo, rows;         // request, its slots, its first packed row, rows x query heads of the tile
+  int b, len, lo, n, rows;      // request, its slots, its first packed row, its rows; rows x query heads of the tile
   int kv_head, row0;            // key head; the tile's first (row x query head)
   int t0, t1;                   // key tiles
   bool whole;                   // the item has no other segment
@@ -126,7 +126,7 @@ struct CachedWalk {
     s.t1 = (int)min((long long)tiles, s.t0 + (w_end - w));
     s.whole = s.t0 == 0 && s.t1 == tiles;
     s.slot = w == w_begin ? 0 : 1;
-    s.b = b; s.len = r.len; s.lo = r.lo;
+    s.b = b; s.len = r.len; s.lo = r.lo; s.n = r.n;
     s.kv_head = item / row_tiles;
     s.row0 = (item - s.kv_head * row_tiles) * a.tile_rows;
     s.rows = (int)min((long long)a.tile_rows, (long long)r.n * a.group - s.row0);
@@ -181,6 +181,19 @@ __device__ __forceinline__ void cached_write_empty(const CachedArgs& a, int tid,
 __device__ __forceinline__ int cached_row_index(const CachedArgs& a, const CachedSegment& s, int r) {
   const int f = s.row0 + r, i = f / a.group;
   return (s.lo + i) * a.H + s.kv_head * a.group + (f - i * a.group);
+}
+
+// Where the raw scores of a request (n rows from packed row lo on, `len` slots) are kept: key tile by key tile, in a tile key head by
+// key head and row x query head by row x query head, 128 keys each (the last tile as many as it has, rounded up to four).  So what a
+// CTA writes per tile is one piece, and what the weights of a tile's slots are summed from is another.  (Row by row of
+// all slots, 512 bytes here and there / so, us: eight blocks of 4 rows x 32 heads 79.8 / 73.3, 4 rows x 32 heads on 8 34.4 / 31.7.)
+struct CachedScores { float* tile; int pitch; };
+__device__ __forceinline__ CachedScores cached_scores(const CachedArgs& a, int lo, int n, int len, int t) {
+  const int left = len - t * kKeyTile;
+  CachedScores s;
+  s.tile = a.scores + (size_t)lo * a.H * a.score_stride + (size_t)t * kKeyTile * (n * a.H);
+  s.pitch = left >= kKeyTile ? kKeyTile : (left + 3) & ~3;
+  return s;
 }
 
 // The slot's place in the pools, -1 where its page is not one of them.
