@@ -62,11 +62,13 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
     const bool scored = a.scores != nullptr && my_row < s.rows;
     float m = -INFINITY, l = 0.f;                // of this lane's row, over its own pairs (l) and all lanes' (m)
     const int end = min(s.len, s.t1 * kKeyTile);
+    // lane i: where key i of a step is (slots of a pool are counted in 31 bits); looked up a step ahead
+    auto find = [&](int key0) { return lane < kKeys && key0 + lane < end ? (int)cached_place(table, key0 + lane, a.page_size, a.pages) : -1; };
+    int next_at = find(s.t0 * kKeyTile + warp * kKeys);
     for (int key0 = s.t0 * kKeyTile + warp * kKeys; key0 < end; key0 += kWarps * kKeys) {
       float val[LPK];
       float4 vv[kAhead];
-      int at = -1;                               // lane i: where key i is (slots of a pool are counted in 31 bits)
-      if (lane < kKeys && key0 + lane < end) at = (int)cached_place(table, key0 + lane, a.page_size, a.pages);
+      const int at = next_at;
       int place[kPasses];
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) place[p] = __shfl_sync(0xffffffffu, at, p * kSide + side);
@@ -80,6 +82,7 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
 #pragma unroll
         for (int p = 0; p < kAhead; ++p)
           kk[p] = place[p0 + p] >= 0 && has ? load4(kp + (size_t)place[p0 + p] * pitch) : make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p0 == 0) next_at = find(key0 + kWarps * kKeys);
 #pragma unroll
         for (int p = 0; p < kAhead; ++p)
 #pragma unroll
