@@ -340,7 +340,8 @@ typedef struct {
  * gradient of a rotation's output to its input).  q [rows, H, dh], k [rows, kv_heads, dh] or NULL (with k_out NULL);
  * positions [rows, axes] int32, any value.  q_out may be q and k_out may be k; otherwise the buffers must not overlap.
  * Angles are exact to 2^-32 of a turn at every position; cosine and sine are rounded to fp32, the result once to the
- * storage type.  All row buffers must be 16-byte aligned. */
+ * storage type.  dh must be a multiple of 4 (fp32) or 8 (bf16), here and in d3tom_cache_append.  All row buffers must be
+ * 16-byte aligned. */
 int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
                const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
                d3tom_stream stream);
@@ -372,7 +373,8 @@ int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache,
  *              neither read nor written
  *  max_rows    host: >= every request's rows;  max_length  host: >= every length[b] (smaller values cost time or cut)
  *  row_weight  [total_rows] fp32 or NULL (all 1)
- *  out         [total_rows, H*dh]; rows of a request without slots are zero
+ *  out         [total_rows, H*dh], not over q; rows of a request without slots are zero
+ * Requests may share pages when they are only read; with a mode that writes weights no two requests of a call may.
  * The weights need scratch of the context's decider scores: total_rows <= max_deciders and max_length <=
  * max_visual_per_request, D3TOM_ERR_WORKSPACE otherwise.  bf16 on the tensor-core path needs page_size % 8 == 0
  * (D3TOM_ERR_UNSUPPORTED otherwise).  q, out, cache->k and cache->v must be 16-byte aligned.

@@ -69,6 +69,15 @@ class Cache:
         self.dt = _dt(k)
         self._struct = _CacheStruct(*(_ptr(t) for t in self.tensors), k.shape[0], k.shape[1], k.shape[2], page_table.shape[1])
         self.ref = C.byref(self._struct)
+        self.batch = page_table.shape[0]
+
+    def check(self, B: int, *rows):
+        """Rows of the cache's type, and a batch that the table has."""
+        if B > self.batch:
+            raise ValueError("the page table has %d requests" % self.batch)
+        for t in rows:
+            if t is not None and t.dtype != self.k.dtype:
+                raise TypeError("rows and cache are of one storage type")
 
 
 class D3tomError(RuntimeError):
@@ -152,6 +161,13 @@ def _stream(stream):
     if stream is None:
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _i32(t: Optional[torch.Tensor], least: int):
+    """Pointer of an int32 array of at least `least` numbers."""
+    if t is not None and (t.dtype != torch.int32 or t.numel() < least):
+        raise TypeError("an int32 array of at least %d numbers is wanted" % least)
+    return _ptr(t)
 
 
 def _raw_stream(stream, device: int) -> int:
@@ -314,25 +330,25 @@ class Context:
 
     # -------------------------------------------------------------- a K/V cache in pages
     def d3tom_rope(self, spec, q, k, positions, rows, kv_heads, q_out, k_out, inverse=False, stream=None):
-        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _ptr(q), _ptr(k), _ptr(positions), rows, kv_heads,
+        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _ptr(q), _ptr(k), _i32(positions, rows * spec.axes), rows, kv_heads,
                                  int(inverse), _ptr(q_out), _ptr(k_out), _raw_stream(stream, self.device)), "d3tom_rope")
 
     def d3tom_cache_append(self, cache, spec, q, k, v, positions, tokens, first_weight, cu_rows, B, total_rows, q_out,
                            stream=None):
-        if cache.dt != _dt(k) or (q is not None and cache.dt != _dt(q)):
-            raise TypeError("rows and cache are of one storage type")
+        cache.check(B, q, k, v, q_out)
         _check(load().d3tom_cache_append(self._h, cache.dt, cache.ref, None if spec is None else C.byref(spec), _ptr(q), _ptr(k),
-                                         _ptr(v), _ptr(positions), _ptr(tokens), _ptr(first_weight), _ptr(cu_rows), B,
+                                         _ptr(v), _i32(positions, 0 if spec is None else total_rows * spec.axes),
+                                         _i32(tokens, total_rows), _ptr(first_weight), _i32(cu_rows, B + 1), B,
                                          total_rows, _ptr(q_out), _raw_stream(stream, self.device)), "d3tom_cache_append")
 
     def d3tom_attn_cached(self, cache, q, cu_rows, B, total_rows, max_rows, max_length, softmax_scale, mode, row_weight, out,
                           stream=None):
-        if cache.dt != _dt(q) or cache.dt != _dt(out):
-            raise TypeError("rows and cache are of one storage type")
-        _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _ptr(q), _ptr(cu_rows), B, total_rows, max_rows,
-                                        max_length, softmax_scale, mode, _ptr(row_weight), _ptr(out), _raw_stream(stream, self.device)),
-               "d3tom_attn_cached")
+        cache.check(B, q, out)
+        _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _ptr(q), _i32(cu_rows, B + 1), B, total_rows, max_rows,
+                                        max_length, softmax_scale, mode, _ptr(row_weight), _ptr(out),
+                                        _raw_stream(stream, self.device)), "d3tom_attn_cached")
 
     def d3tom_cache_evict(self, cache, budget, protect_from, B, max_length, length_out, stream=None):
-        _check(load().d3tom_cache_evict(self._h, cache.dt, cache.ref, _ptr(budget), _ptr(protect_from), B, max_length,
-                                        _ptr(length_out), _raw_stream(stream, self.device)), "d3tom_cache_evict")
+        cache.check(B)
+        _check(load().d3tom_cache_evict(self._h, cache.dt, cache.ref, _i32(budget, B), _i32(protect_from, B), B, max_length,
+                                        _i32(length_out, B), _raw_stream(stream, self.device)), "d3tom_cache_evict")

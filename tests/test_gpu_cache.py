@@ -296,6 +296,33 @@ def test_attention_with_scores_that_grow_along_the_cache(dt, dh):
     check_attention(P, 4, [5, 2], B_.WEIGHT_SET, q=randn((9, 4, dh), dt, 3, 3.0))
 
 
+@pytest.mark.parametrize("mode", [B_.WEIGHT_NONE, B_.WEIGHT_SET])
+def test_attention_of_a_token_with_more_heads_per_key_head_than_a_tile_has_columns(mode):
+    check_attention(Pool([333, 90], 16, 1, 64, BF, seed=24), 144, [1, 2], mode)
+    check_attention(Pool([333, 90], 16, 1, 64, FP, seed=24), 144, [1, 2], mode)
+
+
+def test_two_streams_read_one_cache_at_once():
+    lens = [900, 30, 2000, 411]
+    P = Pool(lens, 16, 2, 64, BF, seed=25)
+    runs = []
+    for rows in ([1] * 4, [40] * 4, [3, 0, 17, 1]):
+        total = sum(rows)
+        ctx = B_.Context(total, 4, 8, 64, 1, 1)
+        q = randn((total, 8, 64), BF, total)
+        out = torch.zeros(total, 512, dtype=BF, device=DEV)
+        args = (P.cache, q, i32(cu(rows)), 4, total, max(rows), 2000, 0.125, B_.WEIGHT_NONE, None)
+        ctx.d3tom_attn_cached(*args, out)
+        runs.append((ctx, args, out, [torch.zeros_like(out) for _ in range(20)], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for i in range(20):
+        for ctx, args, _, outs, stream in runs:
+            ctx.d3tom_attn_cached(*args, outs[i], stream=stream)
+    torch.cuda.synchronize()
+    for ctx, _, out, outs, _ in runs:
+        assert ctx.device_status() == 0 and all(torch.equal(out, x) for x in outs)
+
+
 @pytest.mark.parametrize("dt", [BF, FP])
 def test_attention_of_equal_keys_is_the_mean(dt):
     n, dh = 1000, 64
@@ -523,7 +550,9 @@ def test_refusals():
             fn(*a, **kw)
         assert e.value.status == status
 
-    rope = lambda spec, rows=2, kv=2, qq=q: ctx.d3tom_rope(spec, qq, k, pos, rows, kv, torch.empty_like(qq), torch.empty_like(k))
+    many = i32(np.zeros((20, 3)))
+    rope = lambda spec, rows=2, kv=2, qq=q: ctx.d3tom_rope(spec, qq, k, pos if rows == 3 else many, rows, kv, torch.empty_like(qq),
+                                                           torch.empty_like(k))
     for bad in (B_.RopeSpec([0, 0, 0]), B_.RopeSpec([16, 16, 1]), B_.RopeSpec([40]), B_.RopeSpec([-1, 5]), B_.RopeSpec([8], theta=0.5),
                 B_.RopeSpec([8], theta=float("nan")), B_.RopeSpec([8], pairing=2), B_.RopeSpec([8], ladder=-1)):
         refused(B_.ERR_INVALID_ARG, rope, bad)
@@ -540,7 +569,7 @@ def test_refusals():
     refused(B_.ERR_INVALID_ARG, attn, max_length=-1)
     refused(B_.ERR_INVALID_ARG, attn, mode=3)
     refused(B_.ERR_INVALID_ARG, attn, B=0)
-    refused(B_.ERR_WORKSPACE, attn, B=3)
+    refused(B_.ERR_WORKSPACE, ctx.d3tom_attn_cached, Pool([20, 1, 1], 8, 2, 64, BF).cache, q, i32([0, 2, 2, 2]), 3, 2, 2, 20, 0.1, 0, None, out)
     refused(B_.ERR_WORKSPACE, attn, rows=17)
     refused(B_.ERR_WORKSPACE, attn, mode=1, max_length=33)
     refused(B_.ERR_WORKSPACE, attn, mode=1, rows=5)
@@ -564,6 +593,14 @@ def test_refusals():
         ctx.d3tom_attn_cached(P.cache, q.float(), c1, 1, 2, 2, 20, 0.1, 0, None, out)
     with pytest.raises(ValueError):
         B_.Cache(P.k, P.v, P.weight[:1], None, P.table, P.length)
+    with pytest.raises(ValueError):
+        ctx.d3tom_attn_cached(P.cache, q, i32([0, 1, 2]), 2, 2, 1, 20, 0.1, 0, None, out)      # the table has one request
+    with pytest.raises(TypeError):
+        ctx.d3tom_attn_cached(P.cache, q, c1[:1], 1, 2, 2, 20, 0.1, 0, None, out)
+    with pytest.raises(TypeError):
+        rope(B_.RopeSpec([1, 1, 1]), rows=3)                                 # positions of two rows
+    with pytest.raises(TypeError):
+        ctx.d3tom_cache_evict(P.cache, i32([3]).long(), None, 1, 20, P.length)
     torch.cuda.synchronize()
     assert ctx.device_status() == 0
     for x, y in zip(P.flat(), before):
