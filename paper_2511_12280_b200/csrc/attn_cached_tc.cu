@@ -233,21 +233,22 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       if (seg >= S::kQBufs)
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&q_empty[qb], (uint32_t)(seg / S::kQBufs - 1) & 1u, abort_flag, a.dev_status));
       if (!ok) break;
-      constexpr int kChunks = DH / 8, kAhead = 8;       // 16-byte pieces of a row; loads in flight per lane
-      for (int i0 = lane; i0 < N * kChunks; i0 += 32 * kAhead) {
-        uint4 w[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int r = (i0 + u * 32) / kChunks, c = (i0 + u * 32) % kChunks;
-          w[u] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < s.rows) w[u] = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + (size_t)cached_row_index(a, s, r) * DH)[c];
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int r = (i0 + u * 32) / kChunks, c = (i0 + u * 32) % kChunks;
-          if (r < N) *reinterpret_cast<uint4*>(q_s + qb * S::kQBytes + (c / 8) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = w[u];
-        }
+      // asynchronous copies, so that all of a tile's are under way at once; rows that are not there become zeros.  (With loads through
+      // registers, eight at a time, and a division per row this was 10 us at 128 columns.)
+      constexpr int kChunks = DH / 8, kStep = 32 / kChunks;       // 16-byte pieces of a row; rows per step of the warp
+      const int piece = lane % kChunks, di = kStep / a.group, dg = kStep - di * a.group;
+      int r = lane / kChunks, i = (s.row0 + r) / a.group, g = s.row0 + r - i * a.group;
+      const uint8_t* q = static_cast<const uint8_t*>(a.q) + (size_t)s.kv_head * a.group * DH * 2 + piece * 16;
+      const uint32_t dst = ptx::smem_u32(q_s + qb * S::kQBytes + (piece / 8) * (N * 128));
+#pragma unroll 4
+      for (; r < N; r += kStep) {
+        const bool there = r < s.rows;
+        ptx::cp_async_16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), there ? q + ((size_t)(s.lo + i) * a.H + g) * (DH * 2) : q, there);
+        i += di;
+        g += dg;
+        if (g >= a.group) { g -= a.group; ++i; }
       }
+      ptx::cp_async_wait_all();
       ptx::fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&q_full[qb]);
