@@ -237,16 +237,20 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       // registers, eight at a time, and a division per row this was 10 us at 128 columns.)
       constexpr int kChunks = DH / 8, kStep = 32 / kChunks;       // 16-byte pieces of a row; rows per step of the warp
       const int piece = lane % kChunks, di = kStep / a.group, dg = kStep - di * a.group;
-      int r = lane / kChunks, i = (s.row0 + r) / a.group, g = s.row0 + r - i * a.group;
-      const uint8_t* q = static_cast<const uint8_t*>(a.q) + (size_t)s.kv_head * a.group * DH * 2 + piece * 16;
+      int r = lane / kChunks;
+      const int i = (s.row0 + r) / a.group;
+      int g = s.row0 + r - i * a.group;
+      const size_t token = (size_t)a.H * DH * 2;        // bytes of a packed row, and how far a step goes
+      const uint8_t* src = static_cast<const uint8_t*>(a.q) + (size_t)(s.lo + i) * token + (size_t)(s.kv_head * a.group + g) * (DH * 2) + piece * 16;
+      const size_t on = di * token + (size_t)dg * (DH * 2), wrap = token - (size_t)a.group * (DH * 2);
       const uint32_t dst = ptx::smem_u32(q_s + qb * S::kQBytes + (piece / 8) * (N * 128));
 #pragma unroll 4
       for (; r < N; r += kStep) {
         const bool there = r < s.rows;
-        ptx::cp_async_16(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), there ? q + ((size_t)(s.lo + i) * a.H + g) * (DH * 2) : q, there);
-        i += di;
+        ptx::cp_async_16(dst + r * 128 + (((piece ^ r) & 7) << 4), there ? src : a.q, there);
+        src += on;
         g += dg;
-        if (g >= a.group) { g -= a.group; ++i; }
+        if (g >= a.group) { g -= a.group; src += wrap; }
       }
       ptx::cp_async_wait_all();
       ptx::fence_proxy_async_smem();
@@ -443,26 +447,32 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
           if (s.whole) { if (a.lse != nullptr) a.lse[row_s[col0 + gt]] = make_float2(-negm_s[col0 + gt], sum); }
           else { part[N * DH + col0 + gt] = -negm_s[col0 + gt]; part[N * (DH + 1) + col0 + gt] = sum; }
         }
-        alpha_s[col0 + gt] = s.whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+        alpha_s[col0 + gt] = sum == 0.f ? 0.f : 1.f / sum;
       }
       ptx::mbar_wait(pv_done, (uint32_t)(tile - 1) & 1u, abort_flag, a.dev_status);
       ptx::tc_fence_after_sync();
       ptx::named_sync(bar, 128);
+      constexpr int kOut = kCols < 32 ? kCols : 32;
 #pragma unroll 1
-      for (int i0 = 0; i0 < kCols; i0 += 16) {
+      for (int i0 = 0; i0 < kCols; i0 += kOut) {
         if (i0 >= cols) break;
-        uint32_t o[16];
-        ptx::tmem_ld16(tmem + lane_addr + kColO + col0 + i0, o);
+        uint32_t o[kOut];
+        if constexpr (kOut == 16) ptx::tmem_ld16(tmem + lane_addr + kColO + col0 + i0, o);
+        else ptx::tmem_ld32(tmem + lane_addr + kColO + col0 + i0, o);
         ptx::tmem_wait_ld();
         if (key < DH) {
+          if (s.whole) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int col = col0 + i0 + i;
-            if (i0 + i < cols) {
-              const float v = __uint_as_float(o[i]) * alpha_s[col];
-              if (s.whole) static_cast<__nv_bfloat16*>(a.out)[(size_t)row_s[col] * DH + key] = __float2bfloat16_rn(v);
-              else part[col * DH + key] = v;
+            for (int i = 0; i < kOut; ++i) {
+              const int col = col0 + i0 + i;
+              if (i0 + i < cols)
+                static_cast<__nv_bfloat16*>(a.out)[(size_t)row_s[col] * DH + key] = __float2bfloat16_rn(__uint_as_float(o[i]) * alpha_s[col]);
             }
+          } else {
+            float* to = part + (col0 + i0) * DH + key;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+              if (i0 + i < cols) to[i * DH] = __uint_as_float(o[i]);
           }
         }
       }
