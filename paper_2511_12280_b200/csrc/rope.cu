@@ -3,20 +3,13 @@
 // A pair (a, b) of a head becomes (a cos t - b sin t, a sin t + b cos t), t = position * theta^-e.  A position step is held as a
 // 64-bit fraction of a turn, so position * step is an integer product that wraps around where the angle does: its upper 32
 // bits are the angle to 2^-32 of a turn at every position (in fp32 the product itself would be off by radians from a million on),
-// and sincospif needs no range reduction.  The angles of a row are shared by its heads: a block computes them once into shared
-// memory.  Bound: HBM (every row is read and written once); with few rows, latency.
+// and sincospif needs no range reduction.  The angles of a row are shared by its heads: a warp computes them once.  Bound: HBM (every
+// row is read and written once); with few rows, latency.
 #include "common.cuh"
 
 namespace {
 
-constexpr int kThreads = 256;
-
-template <typename T> __device__ __forceinline__ T rotated_lo(T x, T y, float c, float s) {
-  return Storage<T>::from_float(Storage<T>::to_float(x) * c - Storage<T>::to_float(y) * s);
-}
-template <typename T> __device__ __forceinline__ T rotated_hi(T x, T y, float c, float s) {
-  return Storage<T>::from_float(Storage<T>::to_float(x) * s + Storage<T>::to_float(y) * c);
-}
+constexpr int kRowWarps = 4;
 
 // Where a row goes in the pools; -1: nowhere.
 __device__ __forceinline__ long long row_place(const RotateArgs& a, int row) {
@@ -27,105 +20,137 @@ __device__ __forceinline__ long long row_place(const RotateArgs& a, int row) {
   return page < 0 || page >= a.cache.pages ? -1 : (long long)page * a.cache.page_size + ((int)slot - p * a.cache.page_size);
 }
 
-// One block per row (blockIdx.x); gridDim.y blocks share its heads.  kVector: units of 16 bytes (pairs of halves: 2 x 16, where
-// the number of pairs is a multiple of the vector); otherwise a pair or a copied number at a time.
-template <typename T, bool kVector>
-__global__ void __launch_bounds__(kThreads)
-rotate_rows_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, const bool to_cache) {
-  constexpr int kVec = Storage<T>::kVec;
-  __shared__ float2 turn[64];
-  const int tid = threadIdx.x, row = blockIdx.x;
-  grid_dependency_enter();
-  long long place = -1;                          // where the row goes in the pools
-  if (to_cache) {
-    if (row >= a.cu_rows[a.B]) return;           // (the whole block)
-    place = row_place(a, row);
-    if (place < 0 && tid == 0) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
-    if (tid == 0 && blockIdx.y == 0 && place >= 0) {
+// The angles of a row, for a warp: cosine and sine of pairs lane and lane + 32 (c, s [2]).
+template <typename Turn, typename Axis>
+__device__ __forceinline__ void row_angles(const RotateArgs& a, const RopeTable& t, const Turn& turn, const Axis& axis, int row,
+                                           float (&c)[2], float (&s)[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int pr = (threadIdx.x & 31) + j * 32;
+    c[j] = 1.f; s[j] = 0.f;
+    if (pr < t.pairs) {
+      const long long pos = a.positions[(size_t)row * t.axes + axis[pr]];
+      const int32_t part = (int32_t)(((unsigned long long)pos * turn[pr]) >> 32);    // in 2^-32 of a turn, -1/2 .. 1/2
+      sincospif((float)part * 4.656612873077392578125e-10f, &s[j], &c[j]);           // half turns: part * 2^-31
+      if (a.inverse) s[j] = -s[j];
+    }
+  }
+}
+
+// Where the row goes, for a warp; its weight and token's number are written by the row's first part.
+__device__ __forceinline__ long long row_place_and_marks(const RotateArgs& a, int row, bool first) {
+  const long long place = row_place(a, row);
+  if (first) {
+    if (place < 0) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
+    else {
       if (a.cache.weight != nullptr) a.cache.weight[place] = a.first_weight != nullptr ? a.first_weight[row] : 0.f;
       if (a.tokens != nullptr) a.cache.token[place] = a.tokens[row];
     }
   }
-  if (tid < t.pairs) {
-    const long long pos = a.positions[(size_t)row * t.axes + t.axis[tid]];
-    const int32_t part = (int32_t)(((unsigned long long)pos * t.turn[tid]) >> 32);   // in 2^-32 of a turn, -1/2 .. 1/2
-    float s, c;
-    sincospif((float)part * 4.656612873077392578125e-10f, &s, &c);                   // half turns: part * 2^-31
-    turn[tid] = make_float2(c, a.inverse ? -s : s);
-  }
-  __syncthreads();
+  return place;
+}
 
-  const int pairs = t.pairs, dh = a.dh;
-  const int pair_units = !kVector ? pairs : t.neighbours ? 0 : pairs / kVec;      // units that rotate two places at once
-  const int per_head = !kVector ? dh - pairs : t.neighbours ? dh / kVec : dh / kVec - pair_units;
-  const int rot_units = (a.H + a.kv_heads) * per_head, v_units = a.v != nullptr ? a.kv_heads * (dh / kVec) : 0;
-  for (int u = blockIdx.y * kThreads + tid; u < rot_units + v_units; u += gridDim.y * kThreads) {
-    if (u >= rot_units) {                        // a piece of the value row
-      if (place < 0) continue;
-      const size_t off = (size_t)(u - rot_units) * kVec;
-      *reinterpret_cast<uint4*>(static_cast<T*>(a.cache.v) + (size_t)place * a.kv_heads * dh + off) =
-          *reinterpret_cast<const uint4*>(static_cast<const T*>(a.v) + (size_t)row * a.kv_heads * dh + off);
-      continue;
-    }
-    const int head = u / per_head, i = u - head * per_head;
+// W numbers of type T as one load or store
+template <typename T, int W> struct Pack {
+  static constexpr int kBytes = sizeof(T) * W;
+  T e[W];
+  __device__ __forceinline__ void load(const T* p) { copy(reinterpret_cast<const uint8_t*>(p), reinterpret_cast<uint8_t*>(e)); }
+  __device__ __forceinline__ void store(T* p) const { copy(reinterpret_cast<const uint8_t*>(e), reinterpret_cast<uint8_t*>(p)); }
+  __device__ static __forceinline__ void copy(const uint8_t* src, uint8_t* dst) {
+    if constexpr (kBytes == 16) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
+    else if constexpr (kBytes == 8) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(src);
+    else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(src);
+    else *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(src);
+  }
+};
+
+// Any rotation: a warp takes a row, or a part of its units where there are few rows.  A unit is W numbers of either half of the pairs (or W
+// neighbouring numbers), W the largest power of two up to 16 bytes that divides them; a number between the pairs and the first 16-byte
+// boundary after them; or 16 bytes of what is only copied, values included.
+template <typename T, int W, bool kNeighbours>
+__global__ void __launch_bounds__(kRowWarps * 32)
+rotate_rows_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, const bool to_cache, const int parts) {
+  constexpr int kVec = Storage<T>::kVec;
+  __shared__ unsigned long long turn[64];
+  __shared__ int axis[64];
+  __shared__ float2 angle[kRowWarps][64];
+  if (threadIdx.x < t.pairs) { turn[threadIdx.x] = t.turn[threadIdx.x]; axis[threadIdx.x] = t.axis[threadIdx.x]; }
+  __syncthreads();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, w = blockIdx.x * kRowWarps + warp, row = w / parts, part = w - row * parts;
+  if (row >= a.rows) return;
+  grid_dependency_enter();
+  if (to_cache && row >= a.cu_rows[a.B]) return;
+  if (t.pairs > 0) {
+    float c[2], s[2];
+    row_angles(a, t, turn, axis, row, c, s);
+    angle[warp][lane] = make_float2(c[0], s[0]);
+    angle[warp][lane + 32] = make_float2(c[1], s[1]);
+    __syncwarp();
+  }
+  const long long place = to_cache ? row_place_and_marks(a, row, part == 0 && lane == 0) : row;
+  const int pairs = t.pairs, dh = a.dh, first = (2 * pairs + kVec - 1) / kVec;   // 16-byte pieces of a head that are only copied, from here on
+  const int pair_units = kNeighbours ? 2 * pairs / W : pairs / W, single = first * kVec - 2 * pairs;
+  const int per_head = pair_units + single + dh / kVec - first;
+  const int rot_units = (a.H + a.kv_heads) * per_head, units = rot_units + (a.v != nullptr ? a.kv_heads * (dh / kVec) : 0);
+  const size_t width = (size_t)a.kv_heads * dh;
+  const float2* cs = angle[warp];
+#pragma unroll 2
+  for (int u = part * 32 + lane; u < units; u += parts * 32) {
     const T* src;
     T* dst;
-    if (head < a.H) {
-      const size_t off = ((size_t)row * a.H + head) * dh;
-      src = static_cast<const T*>(a.q) + off;
-      dst = static_cast<T*>(a.q_out) + off;
+    int i = pair_units + single;                 // a copied piece at src
+    if (u >= rot_units) {
+      if (place < 0) continue;
+      const size_t off = (size_t)(u - rot_units) * kVec;
+      src = static_cast<const T*>(a.v) + (size_t)row * width + off;
+      dst = static_cast<T*>(a.cache.v) + (size_t)place * width + off;
     } else {
-      const size_t off = (size_t)(head - a.H) * dh, width = (size_t)a.kv_heads * dh;
-      src = static_cast<const T*>(a.k) + (size_t)row * width + off;
-      if (to_cache) {
-        if (place < 0) continue;
-        dst = static_cast<T*>(a.cache.k) + (size_t)place * width + off;
+      const int head = u / per_head;
+      i = u - head * per_head;
+      if (head < a.H) {
+        const size_t off = ((size_t)row * a.H + head) * dh;
+        src = static_cast<const T*>(a.q) + off;
+        dst = static_cast<T*>(a.q_out) + off;
       } else {
-        dst = static_cast<T*>(a.k_out) + (size_t)row * width + off;
+        if (place < 0) continue;
+        const size_t off = (size_t)(head - a.H) * dh;
+        src = static_cast<const T*>(a.k) + (size_t)row * width + off;
+        dst = static_cast<T*>(to_cache ? a.cache.k : a.k_out) + (size_t)place * width + off;
+      }
+      if (i >= pair_units + single) {
+        const int at = (first + i - pair_units - single) * kVec;
+        src += at; dst += at;
+        i = pair_units + single;
       }
     }
-    if constexpr (!kVector) {
-      if (i < pairs) {
-        const int lo = t.neighbours ? 2 * i : i, hi = t.neighbours ? 2 * i + 1 : pairs + i;
-        const T x = src[lo], y = src[hi];
-        const float2 cs = turn[i];
-        dst[lo] = rotated_lo(x, y, cs.x, cs.y);
-        dst[hi] = rotated_hi(x, y, cs.x, cs.y);
-      } else {
-        dst[pairs + i] = src[pairs + i];
-      }
-    } else if (t.neighbours) {
-      float f[kVec];
-      const uint4 raw = *reinterpret_cast<const uint4*>(src + i * kVec);
-      if (i * kVec >= 2 * pairs) { *reinterpret_cast<uint4*>(dst + i * kVec) = raw; continue; }
-      Storage<T>::load(src + i * kVec, f);
+    if (i >= pair_units + single) {
+      *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
+    } else if (i >= pair_units) {
+      dst[2 * pairs + i - pair_units] = src[2 * pairs + i - pair_units];
+    } else if constexpr (kNeighbours) {
+      Pack<T, W> x;
+      x.load(src + i * W);
 #pragma unroll
-      for (int e = 0; e < kVec; e += 2) {
-        const int pr = (i * kVec + e) >> 1;
-        if (pr < pairs) {
-          const float2 cs = turn[pr];
-          const float x = f[e], y = f[e + 1];
-          f[e] = x * cs.x - y * cs.y;
-          f[e + 1] = x * cs.y + y * cs.x;
-        }
+      for (int e = 0; e < W; e += 2) {
+        const float2 f = cs[(i * W + e) >> 1];
+        const float p = Storage<T>::to_float(x.e[e]), r = Storage<T>::to_float(x.e[e + 1]);
+        x.e[e] = Storage<T>::from_float(p * f.x - r * f.y);
+        x.e[e + 1] = Storage<T>::from_float(p * f.y + r * f.x);
       }
-      Storage<T>::store(dst + i * kVec, f);
-    } else if (i < pair_units) {
-      float x[kVec], y[kVec];
-      Storage<T>::load(src + i * kVec, x);
-      Storage<T>::load(src + pairs + i * kVec, y);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float2 cs = turn[i * kVec + e];
-        const float r = x[e] * cs.x - y[e] * cs.y;
-        y[e] = x[e] * cs.y + y[e] * cs.x;
-        x[e] = r;
-      }
-      Storage<T>::store(dst + i * kVec, x);
-      Storage<T>::store(dst + pairs + i * kVec, y);
+      x.store(dst + i * W);
     } else {
-      const int at = (pair_units + i) * kVec;
-      *reinterpret_cast<uint4*>(dst + at) = *reinterpret_cast<const uint4*>(src + at);
+      Pack<T, W> x, y;
+      x.load(src + i * W);
+      y.load(src + pairs + i * W);
+#pragma unroll
+      for (int e = 0; e < W; ++e) {
+        const float2 f = cs[i * W + e];
+        const float p = Storage<T>::to_float(x.e[e]), r = Storage<T>::to_float(y.e[e]);
+        x.e[e] = Storage<T>::from_float(p * f.x - r * f.y);
+        y.e[e] = Storage<T>::from_float(p * f.y + r * f.x);
+      }
+      x.store(dst + i * W);
+      y.store(dst + pairs + i * W);
     }
   }
 }
@@ -133,7 +158,7 @@ rotate_rows_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, cons
 // Heads that are rotated whole (2 pairs = dh): a warp takes a row, or a part of its heads where there are few rows.  U lanes have a head, a
 // lane always the same pairs of every head, so their cosines and sines stay in registers; 64 bytes of loads per lane are under
 // way at a time (with 128 a wave of blocks does not fit the SMs), the first ones before the angles are known.  Heads of 128 bf16, us, with
-// the kernel above (angles from shared memory for every unit, a barrier per row) / here: 4288 rows x 64 heads 27.8 / 25.7 (5.5 TB/s),
+// a block per row (angles from shared memory for every unit, a barrier) / here: 4288 rows x 64 heads 27.8 / 25.7 (5.5 TB/s),
 // 21629 rows x (64 + 32) appended 201 / 171 (6.2 TB/s).
 constexpr int kHeadWarps = 4;
 
@@ -170,17 +195,8 @@ rotate_heads_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, con
   int h = part * kHeads + lane / U;
   load(h);
   // the angles: lane i has pairs i and i + 32, then every lane collects those of its place in a head
-  float c[2] = {1.f, 1.f}, s[2] = {0.f, 0.f};
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int pr = lane + j * 32;
-    if (pr < t.pairs) {
-      const long long pos = a.positions[(size_t)row * t.axes + axis[pr]];
-      const int32_t x = (int32_t)(((unsigned long long)pos * turn[pr]) >> 32);
-      sincospif((float)x * 4.656612873077392578125e-10f, &s[j], &c[j]);
-      if (a.inverse) s[j] = -s[j];
-    }
-  }
+  float c[2], s[2];
+  row_angles(a, t, turn, axis, row, c, s);
   float cs[kPairs], sn[kPairs];
 #pragma unroll
   for (int e = 0; e < kPairs; ++e) {
@@ -190,17 +206,8 @@ rotate_heads_kernel(const RotateArgs a, const __grid_constant__ RopeTable t, con
     cs[e] = pr < 32 ? c0 : c1;
     sn[e] = pr < 32 ? s0 : s1;
   }
-  long long place = row;                         // of the row in the keys' destination
-  if (to_cache) {
-    place = row_place(a, row);
-    if (part == 0 && lane == 0) {
-      if (place < 0) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
-      else {
-        if (a.cache.weight != nullptr) a.cache.weight[place] = a.first_weight != nullptr ? a.first_weight[row] : 0.f;
-        if (a.tokens != nullptr) a.cache.token[place] = a.tokens[row];
-      }
-    }
-  }
+  // of the row in the keys' destination
+  const long long place = to_cache ? row_place_and_marks(a, row, part == 0 && lane == 0) : row;
   T* q_out = static_cast<T*>(a.q_out) + (size_t)row * a.H * dh + at;
   T* k_out = static_cast<T*>(to_cache ? a.cache.k : a.k_out) + (size_t)(place < 0 ? 0 : place) * width + at;
   for (; h < heads; h += kHeadBatch * step) {
@@ -267,12 +274,18 @@ int launch(d3tom_ctx* ctx, const RotateArgs& a, const RopeTable& t, bool to_cach
     case 32: if (t.neighbours) return launch_heads<T, true, 32>(ctx, a, t, to_cache, s); break;
     default: break;
   }
-  const int units = (a.H + 2 * a.kv_heads) * a.dh / kVec;
-  const int want = ceil_div(2 * ctx->sm_count, a.rows), most = ceil_div(units, kThreads);
-  const dim3 grid(a.rows, want < 1 ? 1 : want < most ? want : most);
-  const bool vector = t.neighbours || t.pairs % kVec == 0;
-  if (vector) D3TOM_CUDA_TRY(ctx, launch_serialized(rotate_rows_kernel<T, true>, grid, kThreads, 0, s, a, t, to_cache));
-  else D3TOM_CUDA_TRY(ctx, launch_serialized(rotate_rows_kernel<T, false>, grid, kThreads, 0, s, a, t, to_cache));
+  // the widest unit that divides the pairs of a half (or the neighbouring numbers)
+  int unit = kVec;
+  while (unit > (t.neighbours ? 2 : 1) && (t.neighbours ? 2 * t.pairs : t.pairs) % unit != 0) unit >>= 1;
+  auto kernel = t.neighbours ? rotate_rows_kernel<T, 2, true> : rotate_rows_kernel<T, 1, false>;
+  if (unit == 8) { if constexpr (kVec == 8) kernel = t.neighbours ? rotate_rows_kernel<T, 8, true> : rotate_rows_kernel<T, 8, false>; }
+  else if (unit == 4) kernel = t.neighbours ? rotate_rows_kernel<T, 4, true> : rotate_rows_kernel<T, 4, false>;
+  else if (unit == 2) kernel = t.neighbours ? rotate_rows_kernel<T, 2, true> : rotate_rows_kernel<T, 2, false>;
+  // warps enough to hide that a lane has one or two loads under way, each with at least four steps after its angles: 4288 rows of
+  // 64 heads, 30 of 64 pairs rotated, 89 us with 24 warps per SM, 56 with 48
+  const int steps = ceil_div((a.H + 2 * a.kv_heads) * a.dh / unit, 32), want = ceil_div(48 * ctx->sm_count, a.rows);
+  const int most = steps < 4 ? 1 : steps / 4, parts = want < most ? want : most;
+  D3TOM_CUDA_TRY(ctx, launch_serialized(kernel, (int)(((long long)a.rows * parts + kRowWarps - 1) / kRowWarps), kRowWarps * 32, 0, s, a, t, to_cache, parts));
   D3TOM_LAUNCH_CHECK(ctx);
   return D3TOM_OK;
 }
