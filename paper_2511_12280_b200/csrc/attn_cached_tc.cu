@@ -41,6 +41,7 @@ template <int DH, int N> struct Shape {
   // bytes), so two of them run side by side where their shared memory allows (64 requests, up to 8192 slots, 32 / 16 heads x 64:
   // 249 -> 205 us; blocks of 32 rows 60 -> 51)
   static constexpr int kPerSm = DH == 64 && N <= 32 ? 2 : 1;
+  static constexpr bool kScores = DH == 128 ? N <= 64 : N == 16;   // whether raw scores ever go out (attn_cached_mass_columns)
   static constexpr int kQBufs = DH * N >= 128 * 128 ? 1 : 2;
   static constexpr int kSlots = DH == 128 ? (N <= 32 ? 6 : 4) : N == 16 ? 6 : N == 32 ? 4 : N == 64 ? 10 : 8;
   static_assert(kSlots % 2 == 0, "K tiles in the even slots, V tiles in the odd ones: no slot has two producers");
@@ -336,23 +337,20 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         if (first) {
           ptx::named_sync(bar, 128);                    // (row_s)
         }
-        // the raw scores leave once P is announced, beside the second product (32 rows x 32 heads 114 -> 110 us), where registers hold
-        // them that long
-        constexpr bool kLate = kCols <= 32;
-        float raw[kLate ? kCols : 1];
-        if constexpr (kLate) {
+        // the raw scores leave once P is announced, beside the second product (32 rows x 32 heads 114 -> 110 us)
+        float raw[S::kScores ? kCols : 1];
+        if constexpr (S::kScores) {
 #pragma unroll
           for (int i = 0; i < kCols; ++i) raw[i] = e[i];
         }
         auto put_scores = [&](auto& x) {
-          if (a.scores == nullptr || !valid) return;
+          if (!S::kScores || a.scores == nullptr || !valid) return;
           const CachedScores sc = cached_scores(a, s.lo, s.n, s.len, t);
           float* at = sc.tile + (size_t)(s.kv_head * s.n * a.group + s.row0 + col0) * sc.pitch + key;
 #pragma unroll
           for (int i = 0; i < kCols; ++i)
             if (i < cols) at[i * sc.pitch] = x[i];
         };
-        if constexpr (!kLate) put_scores(e);
         if (!first) {
           float top = -INFINITY;
 #pragma unroll
@@ -426,7 +424,7 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         ptx::tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(p_full);
-        if constexpr (kLate) put_scores(raw);
+        if constexpr (S::kScores) put_scores(raw);
       }
       // ---- the segment's result
       constexpr int kSum = kCols < 32 ? kCols : 32;
@@ -535,11 +533,11 @@ int launch_columns(d3tom_ctx* ctx, const CachedArgs& a, bool mass, cudaStream_t 
 
 // Whether the mass per slot comes from a second pass over the keys; the columns whose sums are then one number, 0 if not.
 // Per slot and key head the scores are 8 bytes a column, written and read, the keys 2 dh bytes and a pass has its own ramp.  us, scores
-// out / second pass, eight requests of up to 4288 slots: 32 heads x 128, 16 rows 83 / 103, 32 113 / 114, 64 164 / 138; 32 x 64, 16 rows
-// 59 / 63, 24 80 / 74, 32 94 / 77; 32 heads on 8 x 128, 16 rows (64 columns) 56 / 61, 32 (128) 144 / 100.
+// out / second pass, eight requests of up to 4288 slots: 32 heads x 128, 24 rows 98 / 112, 32 108 / 112, 40 137 / 123; 32 x 64, 17 rows
+// 84 / 76, 24 92 / 78; 32 heads on 8 x 64, 5 rows (20 columns) 39 / 35; ten requests of up to 5345, 8 heads on one x 128, 32 rows 86 / 54.
 int attn_cached_mass_columns(const CachedArgs& a) {
   const long long rows = (long long)a.max_rows * a.group;
-  if (8 * rows < 64 + 2 * a.dh) return 0;
+  if (rows < (a.dh == 128 ? 40 : 17)) return 0;
   if (a.dh == 128) return rows <= 32 ? Shape<128, 32>::kCols : rows <= 64 ? Shape<128, 64>::kCols : Shape<128, 128>::kCols;
   return rows <= 32 ? Shape<64, 32>::kCols : rows <= 64 ? Shape<64, 64>::kCols : Shape<64, 128>::kCols;
 }
