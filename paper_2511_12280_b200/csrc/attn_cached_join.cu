@@ -3,7 +3,8 @@
 //
 // Join: with (O_i, M_i, l_i) of the segments of an item, M = max M_i, l = sum l_i 2^(M_i - M), O = sum O_i 2^(M_i - M) / l.
 // Weight of slot j: sum over the rows i and query heads h of f_i 2^(s_ihj c - M_ih) / l_ih, from the raw scores that the attention
-// kernel left (they are 1 / (64 kv_heads / heads) of the keys' bytes).  Both in a fixed order.  Bound: latency, then HBM.
+// kernel left (weight_kernel: HBM, 88 MB in 20 us; latency where they are few) or from what its second pass summed already (mass_kernel:
+// latency).  All in a fixed order.
 #include "cache_walk.cuh"
 #include "ptx.cuh"
 
@@ -144,8 +145,8 @@ int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a,
 int launch_cached_weight(d3tom_ctx* ctx, const CachedArgs& a, float* weight, int add, int mass_columns, cudaStream_t s) {
   const int chunks = ceil_div(a.cap, 128);
   if ((long long)chunks * a.B > 0x7fffffffll) return D3TOM_ERR_UNSUPPORTED;
-  // few rows: small blocks, many of them on an SM (64 requests of one row x 32 heads: 14 us with 8 warps, 30 with 16); many
-  // rows: the loads of a block side by side (32 rows x 32 heads: 80 us with 8 warps one after the other, 21 with 16)
+  // few rows: small blocks, many of them on an SM (64 requests of one row x 32 heads: 14 us with 4 warps, 30 with 16); many rows: the
+  // loads of a block side by side (32 rows x 32 heads: 21 us with 16 warps, eight loads each under way; 80 with 8 warps and one)
   if (mass_columns > 0) D3TOM_CUDA_TRY(ctx, launch_serialized(mass_kernel, chunks * a.B, 128, 0, s, a, weight, add, chunks, mass_columns));
   else if ((long long)a.max_rows * a.H <= 256) D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<4>, chunks * a.B, 4 * 32, 0, s, a, weight, add, chunks));
   else D3TOM_CUDA_TRY(ctx, launch_serialized(weight_kernel<16>, chunks * a.B, 16 * 32, 0, s, a, weight, add, chunks));

@@ -241,8 +241,8 @@ struct CachedArgs {
   int B, H, dh, kv_heads, group, total_rows, max_rows;
   int pages, page_size, max_pages, cap;   // cap: slots a request can have in this call
   float scale_log2;             // softmax_scale * log2(e)
-  float* scores; float2* lse; int score_stride;   // [total_rows][H][score_stride] raw q.k and [total_rows][H] (M, l); null without weights
-  const float* row_weight; float* mass;     // second pass over the keys: [total_rows] or null; sums, at the scores' place
+  float* scores; float2* lse; int score_stride;   // raw q.k (cache_walk.cuh), up to score_stride per row x head, and [total_rows][H] (M, l); null without weights
+  const float* row_weight; float* mass;     // [total_rows] or null; sums of a second pass over the keys, [total_rows * H][score_stride] at the scores' place
   float* part;                  // [ctas][2] parts of work items that several CTAs share (cache_walk.cuh)
   int* joins;                   // [ctas][8] what the join has to do
   int tile_rows, ctas, read_once;   // set by the launcher; read_once: no item shares its keys with another
