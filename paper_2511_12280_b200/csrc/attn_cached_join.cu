@@ -135,6 +135,7 @@ mass_kernel(const CachedArgs a, float* __restrict__ weight, const int add, const
 }  // namespace
 
 int launch_attn_cached_join(d3tom_ctx* ctx, d3tom_dtype dt, const CachedArgs& a, cudaStream_t s) {
+  if (a.cap <= kKeyTile) return D3TOM_OK;        // no item has a second tile
   const dim3 grid(a.ctas, ceil_div(a.tile_rows, kJoinWarps));
   if (dt == D3TOM_BF16) D3TOM_CUDA_TRY(ctx, launch_serialized(join_kernel<__nv_bfloat16>, grid, kJoinWarps * 32, 0, s, a));
   else D3TOM_CUDA_TRY(ctx, launch_serialized(join_kernel<float>, grid, kJoinWarps * 32, 0, s, a));

@@ -6,13 +6,14 @@
 //   S^T [128 keys x N] = K Q^T        A = a tile of K as it lies in the cache, B = the rows of Q
 //   O^T [dh x N]      += V^T P^T      A = a tile of V, read along dh (its transpose costs nothing), B = P in shared memory
 // and no part of a tile is padding but the columns between the rows there are and the next of 16, 32, 64, 128.  The cache is read
-// once, by TMA, a page (or its largest power-of-two part) per copy, through a ring of up to twelve tiles that runs ahead across
-// work items: bound by HBM up to 64 columns, by exponentials and shared memory at 128.
+// once, by TMA, a page (or its largest power-of-two part) per copy, through a ring of four to ten tiles that runs ahead across work
+// items: bound by HBM up to 64 columns (one token of 131071 slots x 8 key heads x 128 in 89 us, 6.0 TB/s), by exponentials and
+// shared memory at 128.
 //
 // Softmax over the keys is a sum over lanes here.  A thread has one key's scores of all columns; the running maximum is only a
 // reference that has to lie within 2^8 of the true one (exact after the final division), so a tile costs one barrier that asks
 // whether any score outgrew it, and only a segment's first tile and the rare one that did take maxima over the lanes.  Sums stay
-// per lane until the segment ends.  Scores, maxima and sums are fp32; P is rounded to bf16 for the second product (2^-9 of
+// per lane until the segment ends.  Scores, maxima and sums are fp32; P is rounded to bf16 for the second product (2^-8 of
 // each term at most, unbiased), as in the other attention kernels.
 //
 // The mass per slot.  With few columns the raw scores go out (4 bytes per column, slot and key head, written and read again) and a
@@ -22,7 +23,7 @@
 //
 //   warps 0 .. 3 (or 0 .. 7, a half of the columns each)  softmax and epilogue, a key / a number of O per thread
 //   then one warp each: MMA issue, Q rows into shared memory, TMA producer of K, TMA producer of V
-// One CTA per SM walks its run of key tiles (cache_walk.cuh).  Every wait is bounded; after one that ran out the softmax
+// A CTA per SM (two at head_dim 64 up to 32 columns) walks its run of key tiles (cache_walk.cuh).  Every wait is bounded; after one that ran out the softmax
 // warps go through the rest of their run without waiting (their barriers need all of them), the other warps stop.
 #include "cache_walk.cuh"
 #include "ptx.cuh"
