@@ -71,13 +71,12 @@ class Cache:
         self.ref = C.byref(self._struct)
         self.batch = page_table.shape[0]
 
-    def check(self, B: int, *rows):
-        """Rows of the cache's type, and a batch that the table has."""
+    def check(self, B: int, head_dim: int):
+        """A batch that the table has, and the context's head size."""
         if B > self.batch:
             raise ValueError("the page table has %d requests" % self.batch)
-        for t in rows:
-            if t is not None and t.dtype != self.k.dtype:
-                raise TypeError("rows and cache are of one storage type")
+        if self.k.shape[3] != head_dim:
+            raise ValueError("a cache of head_dim %d under a context of %d" % (self.k.shape[3], head_dim))
 
 
 class D3tomError(RuntimeError):
@@ -167,6 +166,20 @@ def _i32(t: Optional[torch.Tensor], least: int):
     """Pointer of an int32 array of at least `least` numbers."""
     if t is not None and (t.dtype != torch.int32 or t.numel() < least):
         raise TypeError("an int32 array of at least %d numbers is wanted" % least)
+    return _ptr(t)
+
+
+def _f32(t: Optional[torch.Tensor], least: int):
+    """Pointer of an fp32 array of at least `least` numbers."""
+    if t is not None and (t.dtype != torch.float32 or t.numel() < least):
+        raise TypeError("an fp32 array of at least %d numbers is wanted" % least)
+    return _ptr(t)
+
+
+def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, count: int):
+    """Pointer of rows of a storage type, at least `count` numbers of them."""
+    if t is not None and (t.dtype != dtype or t.numel() < count):
+        raise TypeError("at least %d numbers of %s are wanted, as rows of the call's storage type" % (count, dtype))
     return _ptr(t)
 
 
@@ -329,26 +342,41 @@ class Context:
                                 _stream(stream)), "d3tom_ffn")
 
     # -------------------------------------------------------------- a K/V cache in pages
+    def _row_numbers(self, rows: int, limit: int) -> int:
+        """Numbers per head of `rows` rows that a call has to be given; none where the library refuses so many as beyond the
+        context's limits."""
+        return rows * self.limits.head_dim if rows <= limit else 0
+
     def d3tom_rope(self, spec, q, k, positions, rows, kv_heads, q_out, k_out, inverse=False, stream=None):
-        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _ptr(q), _ptr(k), _i32(positions, rows * spec.axes), rows, kv_heads,
-                                 int(inverse), _ptr(q_out), _ptr(k_out), _raw_stream(stream, self.device)), "d3tom_rope")
+        lim, dt = self.limits, q.dtype
+        head = self._row_numbers(rows, lim.max_total_tokens)
+        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _rows(q, dt, head * lim.heads), _rows(k, dt, head * kv_heads),
+                                 _i32(positions, rows * spec.axes), rows, kv_heads, int(inverse), _rows(q_out, dt, head * lim.heads),
+                                 _rows(k_out, dt, head * kv_heads), _raw_stream(stream, self.device)), "d3tom_rope")
 
     def d3tom_cache_append(self, cache, spec, q, k, v, positions, tokens, first_weight, cu_rows, B, total_rows, q_out,
                            stream=None):
-        cache.check(B, q, k, v, q_out)
-        _check(load().d3tom_cache_append(self._h, cache.dt, cache.ref, None if spec is None else C.byref(spec), _ptr(q), _ptr(k),
-                                         _ptr(v), _i32(positions, 0 if spec is None else total_rows * spec.axes),
-                                         _i32(tokens, total_rows), _ptr(first_weight), _i32(cu_rows, B + 1), B,
-                                         total_rows, _ptr(q_out), _raw_stream(stream, self.device)), "d3tom_cache_append")
+        lim, dt = self.limits, cache.k.dtype
+        cache.check(B, lim.head_dim)
+        head = self._row_numbers(total_rows, lim.max_total_tokens)
+        of_q, of_kv = head * lim.heads, head * cache.k.shape[2]
+        _check(load().d3tom_cache_append(self._h, cache.dt, cache.ref, None if spec is None else C.byref(spec), _rows(q, dt, of_q),
+                                         _rows(k, dt, of_kv), _rows(v, dt, of_kv),
+                                         _i32(positions, 0 if spec is None else total_rows * spec.axes),
+                                         _i32(tokens, total_rows), _f32(first_weight, total_rows), _i32(cu_rows, B + 1), B,
+                                         total_rows, _rows(q_out, dt, of_q), _raw_stream(stream, self.device)), "d3tom_cache_append")
 
     def d3tom_attn_cached(self, cache, q, cu_rows, B, total_rows, max_rows, max_length, softmax_scale, mode, row_weight, out,
                           stream=None):
-        cache.check(B, q, out)
-        _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _ptr(q), _i32(cu_rows, B + 1), B, total_rows, max_rows,
-                                        max_length, softmax_scale, mode, _ptr(row_weight), _ptr(out),
+        lim, dt = self.limits, cache.k.dtype
+        cache.check(B, lim.head_dim)
+        of_q = lim.heads * self._row_numbers(total_rows, lim.max_total_tokens if mode == WEIGHT_NONE else
+                                             min(lim.max_total_tokens, lim.max_deciders))
+        _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _rows(q, dt, of_q), _i32(cu_rows, B + 1), B, total_rows, max_rows,
+                                        max_length, softmax_scale, mode, _f32(row_weight, total_rows), _rows(out, dt, of_q),
                                         _raw_stream(stream, self.device)), "d3tom_attn_cached")
 
     def d3tom_cache_evict(self, cache, budget, protect_from, B, max_length, length_out, stream=None):
-        cache.check(B)
+        cache.check(B, self.limits.head_dim)
         _check(load().d3tom_cache_evict(self._h, cache.dt, cache.ref, _i32(budget, B), _i32(protect_from, B), B, max_length,
                                         _i32(length_out, B), _raw_stream(stream, self.device)), "d3tom_cache_evict")
