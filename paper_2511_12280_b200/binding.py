@@ -66,7 +66,8 @@ class Cache:
                 raise ValueError("weight (fp32) and token (int32) are [pages, page_size]")
         self.tensors = (k, v, weight, token, page_table, length)
         self.k, self.v, self.weight, self.token, self.page_table, self.length = self.tensors
-        self.dt = _dt(k)
+        self.dt, self.dtype = _dt(k), k.dtype
+        self.kv_heads, self.head_dim = k.shape[2], k.shape[3]
         self._struct = _CacheStruct(*(_ptr(t) for t in self.tensors), k.shape[0], k.shape[1], k.shape[2], page_table.shape[1])
         self.ref = C.byref(self._struct)
         self.batch = page_table.shape[0]
@@ -75,8 +76,8 @@ class Cache:
         """A batch that the table has, and the context's head size."""
         if B > self.batch:
             raise ValueError("the page table has %d requests" % self.batch)
-        if self.k.shape[3] != head_dim:
-            raise ValueError("a cache of head_dim %d under a context of %d" % (self.k.shape[3], head_dim))
+        if self.head_dim != head_dim:
+            raise ValueError("a cache of head_dim %d under a context of %d" % (self.head_dim, head_dim))
 
 
 class D3tomError(RuntimeError):
@@ -177,10 +178,13 @@ def _f32(t: Optional[torch.Tensor], least: int):
 
 
 def _rows(t: Optional[torch.Tensor], dtype: torch.dtype, count: int):
-    """Pointer of rows of a storage type, at least `count` numbers of them."""
-    if t is not None and (t.dtype != dtype or t.numel() < count):
+    """Pointer of rows of a storage type, at least `count` numbers of them.  (_ptr written out: on the way of every small call.)"""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < count:
         raise TypeError("at least %d numbers of %s are wanted, as rows of the call's storage type" % (count, dtype))
-    return _ptr(t)
+    assert t.is_cuda and t.is_contiguous(), "device, contiguous tensors only"
+    return t.data_ptr()
 
 
 def _raw_stream(stream, device: int) -> int:
@@ -260,6 +264,8 @@ class Context:
         self._h = C.c_void_p()
         self.limits = Limits(max_total_tokens, max_batch, heads, head_dim, max_deciders, max_visual_per_request)
         self.device = device
+        self._heads, self._dh, self._most_rows = heads, head_dim, max_total_tokens
+        self._most_scored = min(max_total_tokens, max_deciders)
         _check(load().d3tom_create(C.byref(self._h), device, C.byref(self.limits)), "d3tom_create")
 
     def close(self):
@@ -342,24 +348,19 @@ class Context:
                                 _stream(stream)), "d3tom_ffn")
 
     # -------------------------------------------------------------- a K/V cache in pages
-    def _row_numbers(self, rows: int, limit: int) -> int:
-        """Numbers per head of `rows` rows that a call has to be given; none where the library refuses so many as beyond the
-        context's limits."""
-        return rows * self.limits.head_dim if rows <= limit else 0
-
+    # (numbers of rows that are beyond the context's limits are not asked for: the library refuses those calls itself)
     def d3tom_rope(self, spec, q, k, positions, rows, kv_heads, q_out, k_out, inverse=False, stream=None):
-        lim, dt = self.limits, q.dtype
-        head = self._row_numbers(rows, lim.max_total_tokens)
-        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _rows(q, dt, head * lim.heads), _rows(k, dt, head * kv_heads),
-                                 _i32(positions, rows * spec.axes), rows, kv_heads, int(inverse), _rows(q_out, dt, head * lim.heads),
-                                 _rows(k_out, dt, head * kv_heads), _raw_stream(stream, self.device)), "d3tom_rope")
+        dt, per_head = q.dtype, rows * self._dh if rows <= self._most_rows else 0
+        of_q, of_k = per_head * self._heads, per_head * kv_heads
+        _check(load().d3tom_rope(self._h, _dt(q), C.byref(spec), _rows(q, dt, of_q), _rows(k, dt, of_k), _i32(positions, rows * spec.axes),
+                                 rows, kv_heads, int(inverse), _rows(q_out, dt, of_q), _rows(k_out, dt, of_k),
+                                 _raw_stream(stream, self.device)), "d3tom_rope")
 
     def d3tom_cache_append(self, cache, spec, q, k, v, positions, tokens, first_weight, cu_rows, B, total_rows, q_out,
                            stream=None):
-        lim, dt = self.limits, cache.k.dtype
-        cache.check(B, lim.head_dim)
-        head = self._row_numbers(total_rows, lim.max_total_tokens)
-        of_q, of_kv = head * lim.heads, head * cache.k.shape[2]
+        cache.check(B, self._dh)
+        dt, per_head = cache.dtype, total_rows * self._dh if total_rows <= self._most_rows else 0
+        of_q, of_kv = per_head * self._heads, per_head * cache.kv_heads
         _check(load().d3tom_cache_append(self._h, cache.dt, cache.ref, None if spec is None else C.byref(spec), _rows(q, dt, of_q),
                                          _rows(k, dt, of_kv), _rows(v, dt, of_kv),
                                          _i32(positions, 0 if spec is None else total_rows * spec.axes),
@@ -368,15 +369,14 @@ class Context:
 
     def d3tom_attn_cached(self, cache, q, cu_rows, B, total_rows, max_rows, max_length, softmax_scale, mode, row_weight, out,
                           stream=None):
-        lim, dt = self.limits, cache.k.dtype
-        cache.check(B, lim.head_dim)
-        of_q = lim.heads * self._row_numbers(total_rows, lim.max_total_tokens if mode == WEIGHT_NONE else
-                                             min(lim.max_total_tokens, lim.max_deciders))
+        cache.check(B, self._dh)
+        dt, most = cache.dtype, self._most_rows if mode == WEIGHT_NONE else self._most_scored
+        of_q = total_rows * self._heads * self._dh if total_rows <= most else 0
         _check(load().d3tom_attn_cached(self._h, cache.dt, cache.ref, _rows(q, dt, of_q), _i32(cu_rows, B + 1), B, total_rows, max_rows,
                                         max_length, softmax_scale, mode, _f32(row_weight, total_rows), _rows(out, dt, of_q),
                                         _raw_stream(stream, self.device)), "d3tom_attn_cached")
 
     def d3tom_cache_evict(self, cache, budget, protect_from, B, max_length, length_out, stream=None):
-        cache.check(B, self.limits.head_dim)
+        cache.check(B, self._dh)
         _check(load().d3tom_cache_evict(self._h, cache.dt, cache.ref, _i32(budget, B), _i32(protect_from, B), B, max_length,
                                         _i32(length_out, B), _raw_stream(stream, self.device)), "d3tom_cache_evict")
