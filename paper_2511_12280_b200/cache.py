@@ -42,14 +42,21 @@ class PagedCache:
         self.free = list(range(pages - 1, -1, -1))
         self.scale = 1.0 / float(np.sqrt(head_dim))
 
+    def _of_requests(self, numbers: Sequence[int], least: Optional[int] = 0):
+        """A number for every request, none below `least`."""
+        if len(numbers) != self.batch or (least is not None and min(numbers) < least):
+            raise ValueError("%d numbers are wanted, one for every request, not below %s: %s" % (self.batch, least, list(numbers)))
+        return numbers
+
     def _resize(self, lengths: Sequence[int]):
-        """Pages for the new lengths; table and lengths on the device follow in stream order."""
+        """Pages for the new lengths; table and lengths on the device follow in stream order.  Pages are given back in the
+        reverse of the order they were taken in: a growth that is taken back leaves everything as it was."""
         need = [-(-n // self.page_size) for n in lengths]
         have = [-(-n // self.page_size) for n in self.lengths_h]
         if max(lengths) > self.max_length or sum(max(0, n - h) for n, h in zip(need, have)) > len(self.free):
             raise RuntimeError("the cache is full: %s slots asked for" % (list(lengths),))
-        for b, (n, h) in enumerate(zip(need, have)):
-            for p in range(n, h):
+        for b, (n, h) in reversed(list(enumerate(zip(need, have)))):
+            for p in range(h - 1, n - 1, -1):
                 self.free.append(int(self.table_h[b, p]))
                 self.table_h[b, p] = -1
         for b, (n, h) in enumerate(zip(need, have)):
@@ -66,24 +73,30 @@ class PagedCache:
     def append(self, rows: Sequence[int], k, v, tokens, q=None, q_out=None, spec: Optional[B_.RopeSpec] = None,
                positions=None, first_weight=None):
         """Writes rows[b] new rows of every request behind its slots; q rotated alike goes to q_out.  first_weight +inf
-        keeps a row from being evicted."""
-        if len(rows) != self.batch:
-            raise ValueError("rows of every request")
-        self._resize([n + r for n, r in zip(self.lengths_h, rows)])
-        self.ctx.d3tom_cache_append(self.cache, spec, q, k, v, positions, tokens, first_weight, self._cu(rows), self.batch,
-                                    int(sum(rows)), q_out)
+        keeps a row from being evicted.  A call that is refused leaves lengths and pages as they were."""
+        before = self.lengths_h
+        self._resize([n + r for n, r in zip(before, self._of_requests(rows))])
+        try:
+            self.ctx.d3tom_cache_append(self.cache, spec, q, k, v, positions, tokens, first_weight, self._cu(rows), self.batch,
+                                        int(sum(rows)), q_out)
+        except BaseException:
+            self._resize(before)
+            raise
 
     def attend(self, rows: Sequence[int], q, out, mode: int = B_.WEIGHT_NONE, row_weight=None):
         """Attention of rows[b] rows of every request over all of its slots."""
+        self._of_requests(rows)
         self.ctx.d3tom_attn_cached(self.cache, q, self._cu(rows), self.batch, int(sum(rows)), max(rows), max(self.lengths_h),
                                    self.scale, mode, row_weight, out)
 
     def evict(self, budget: Sequence[int], protect_from=None):
         """Keeps the min(budget[b], length) heaviest slots of every request; frees the pages behind them."""
-        want = torch.as_tensor(np.asarray(budget, dtype=np.int32), device=self.dev)
+        want = torch.as_tensor(np.asarray(self._of_requests(budget, None), dtype=np.int32), device=self.dev)
         self.ctx.d3tom_cache_evict(self.cache, want, protect_from, self.batch, max(self.lengths_h), self.length)
         self._resize([min(max(int(x), 0), n) for x, n in zip(budget, self.lengths_h)])
 
     def drop_last(self, rows: Sequence[int]):
-        """Gives up the last rows[b] slots of every request (a block that the next step writes again)."""
-        self._resize([n - r for n, r in zip(self.lengths_h, rows)])
+        """Gives up the last rows[b] slots of every request (a block that the next step writes again).  Before an eviction: that
+        one moves kept slots, and the last ones are the block's no longer."""
+        left = [n - r for n, r in zip(self.lengths_h, self._of_requests(rows))]
+        self._resize(self._of_requests(left))
