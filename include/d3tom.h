@@ -353,7 +353,8 @@ int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, cons
  *  k, v       [total_rows, kv_heads, dh]
  *  positions  [total_rows, axes] int32 (NULL without spec)
  *  tokens     [total_rows] int32 numbers for cache->token (NULL: cache->token is left alone)
- *  first_weight  [total_rows] fp32 for cache->weight (NULL: 0); +inf keeps a slot from being evicted
+ *  first_weight  [total_rows] fp32 for cache->weight (NULL: 0); +inf keeps a slot from being evicted for as long as it is
+ *             there: no mode of d3tom_attn_cached takes it away
  *  cu_rows    [B+1] int32, prefix sum of the new rows; total_rows == cu_rows[B] (host copy); rows behind cu_rows[B]
  *             are neither read nor written
  * Two rows of one call must not have the same slot.  A row whose slot does not exist is dropped (see d3tom_attn_cached).
@@ -368,7 +369,8 @@ int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache,
  * With mode D3TOM_WEIGHT_ADD / D3TOM_WEIGHT_SET the attention mass of every slot,
  *   mass_j = sum_i row_weight_i sum_h A_ihj,
  * is added to / stored in cache->weight (the importance of Sec. 3.2.1, S_j, when the rows are the deciders, or
- * row_weight is 1 for deciders and 0 for the others).  Sums run in a fixed order: results are run-to-run identical.
+ * row_weight is 1 for deciders and 0 for the others); a weight of +inf stays.  The mass is 0 in a request without rows, and
+ * D3TOM_WEIGHT_SET stores that too.  Sums run in a fixed order: results are run-to-run identical.
  *  q           [total_rows, H, dh]; rows [cu_rows[b], cu_rows[b+1]) belong to request b; rows behind cu_rows[B] are
  *              neither read nor written
  *  max_rows    host: >= every request's rows;  max_length  host: >= every length[b] (smaller values cost time or cut)
