@@ -382,7 +382,7 @@ int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache,
  * (D3TOM_ERR_UNSUPPORTED otherwise).  q, out, cache->k and cache->v must be 16-byte aligned.
  * What the device finds wrong: a slot behind max_length or behind the table, or on a page outside [0, pages), does not
  * exist for this call and the other two (it is not read, written or moved), a negative length is 0, and the status word
- * (d3tom_device_status) says D3TOM_ERR_INVALID_ARG. */
+ * (d3tom_device_status) says D3TOM_ERR_INVALID_ARG, unless it says D3TOM_ERR_TIMEOUT. */
 int d3tom_attn_cached(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const void* q, const int32_t* cu_rows,
                       int B, int total_rows, int max_rows, int max_length, float softmax_scale, d3tom_weight_mode mode,
                       const float* row_weight, void* out, d3tom_stream stream);

@@ -143,7 +143,7 @@ attn_cached_tc_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
       int row = find(s.t0);
       for (int t = s.t0; t < s.t1; ++t, ++tile) {
         const uint32_t bad = __ballot_sync(0xffffffffu, row < 0);
-        if (row < 0) { row = outside; atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG); }
+        if (row < 0) { row = outside; report_invalid(a.dev_status); }
         const int next_row = t + 1 < s.t1 ? find(t + 1) : outside;
         ok = __all_sync(0xffffffffu, ptx::mbar_wait(&kv_empty[ring], phase, abort_flag, a.dev_status));
         if (!ok) break;

@@ -40,7 +40,7 @@ struct EvictRequest {
   __device__ __forceinline__ EvictRequest(const EvictArgs& args, int b) : a(args) {
     const int raw = a.cache.length[b];
     n = min(max(raw, 0), a.cap);
-    if (threadIdx.x == 0 && raw != n) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
+    if (threadIdx.x == 0 && raw != n) report_invalid(a.dev_status);
     keep = min(max(a.budget[b], 0), n);
     table = a.cache.page_table + (size_t)b * a.cache.max_pages;
     safe_from = a.protect_from != nullptr ? a.protect_from[b] : 0;
@@ -50,7 +50,7 @@ struct EvictRequest {
     return page < 0 || page >= a.cache.pages ? -1 : page * a.cache.page_size + (slot - p * a.cache.page_size);
   }
   __device__ __forceinline__ uint32_t key_at(int place) const {
-    if (place < 0) { atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG); return 0u; }
+    if (place < 0) { report_invalid(a.dev_status); return 0u; }
     return evict_key(a.cache.weight[place], a.protect_from != nullptr && a.cache.token[place] >= safe_from);
   }
 };

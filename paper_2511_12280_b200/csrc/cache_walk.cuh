@@ -169,7 +169,7 @@ __device__ __forceinline__ void cached_write_empty(const CachedArgs& a, int tid,
   for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
     const CachedRequest r = cached_request(a, b);
     const int raw = a.length[b];
-    if (tid == 0 && (raw < 0 || raw > a.cap)) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
+    if (tid == 0 && (raw < 0 || raw > a.cap)) report_invalid(a.dev_status);
     if (r.len > 0) continue;
     T* out = static_cast<T*>(a.out) + (size_t)r.lo * a.H * a.dh;
     const size_t count = (size_t)r.n * a.H * a.dh;

@@ -151,6 +151,9 @@ template <> struct Storage<__nv_bfloat16> {
   __device__ static __forceinline__ __nv_bfloat16 from_float(float x) { return __float2bfloat16_rn(x); }
 };
 
+// What a kernel finds wrong with its arguments.  The smallest number stays: a wait that ran out is not hidden by it.
+__device__ __forceinline__ void report_invalid(int* dev_status) { atomicMin(dev_status, D3TOM_ERR_INVALID_ARG); }
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -41,7 +41,7 @@ __device__ __forceinline__ void row_angles(const RotateArgs& a, const RopeTable&
 __device__ __forceinline__ long long row_place_and_marks(const RotateArgs& a, int row, bool first) {
   const long long place = row_place(a, row);
   if (first) {
-    if (place < 0) atomicExch(a.dev_status, D3TOM_ERR_INVALID_ARG);
+    if (place < 0) report_invalid(a.dev_status);
     else {
       if (a.cache.weight != nullptr) a.cache.weight[place] = a.first_weight != nullptr ? a.first_weight[row] : 0.f;
       if (a.tokens != nullptr) a.cache.token[place] = a.tokens[row];

@@ -44,3 +44,33 @@ def test_slots_that_are_kept_from_eviction_stay_so_when_weights_are_written(dt, 
         kept = t1[torch.as_tensor(P.at[b][: budget[b]], device=DEV)].tolist()
         assert set(safe[b].tolist()) <= set(kept)
     assert ctx.device_status() == 0
+
+
+# ------------------------------------------------------------------ the status word
+@pytest.mark.parametrize("call", ["append", "attend", "attend_fp32", "length", "evict", "evict_length"])
+def test_a_slot_that_is_not_there_does_not_hide_a_wait_that_ran_out(call):
+    P = Pool([40], 8, 1, 64, FP if call == "attend_fp32" else BF, seed=32)
+    ctx = B_.Context(64, 1, 1, 64, 4, 64)
+    k, out, one = randn((1, 1, 64), P.dt, 1), torch.zeros(1, 64, dtype=P.dt, device=DEV), i32([0, 1])
+    if "length" in call:
+        P.length[0] = 10 ** 6
+    else:
+        P.table[0] = P.pages
+
+    def bad():
+        if call == "append":
+            ctx.d3tom_cache_append(P.cache, None, None, k, k, None, None, None, one, 1, 1, None)
+        elif "evict" in call:
+            ctx.d3tom_cache_evict(P.cache, i32([8]), None, 1, 40, i32([0]))
+        else:
+            ctx.d3tom_attn_cached(P.cache, k, one, 1, 1, 1, 40, 0.125, B_.WEIGHT_SET, None, out)
+
+    if call != "attend_fp32":                    # (the CUDA-core kernel leaves slots out without a word; the lengths are looked at)
+        bad()
+        assert ctx.device_status() == B_.ERR_INVALID_ARG
+    ctx.reset_device_status()
+    ctx.selftest_wait_timeout(10 ** 6)
+    bad()
+    assert ctx.device_status() == B_.ERR_TIMEOUT
+    ctx.reset_device_status()
+    assert ctx.device_status() == 0
