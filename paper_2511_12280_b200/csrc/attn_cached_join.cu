@@ -59,8 +59,13 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const CachedArgs 
   if (lane == 0 && a.lse != nullptr) a.lse[row] = make_float2(m, l);
 }
 
-// What mass `t` makes of a slot's weight.  +inf, which keeps a slot from being evicted, stays when weights are set.
-__device__ __forceinline__ float new_weight(float had, float t, int add) { return add ? had + t : had == INFINITY ? had : t; }
+// Mass `t` into the weight of a request's slot.  +inf, which keeps a slot from being evicted, stays when weights are set.
+__device__ __forceinline__ void put_weight(const CachedArgs& a, float* weight, int b, int slot, float t, int add) {
+  const long long place = cached_place(a.page_table + (size_t)b * a.max_pages, slot, a.page_size, a.pages);
+  if (place < 0) { report_invalid(a.dev_status); return; }
+  const float had = weight[place];
+  weight[place] = add ? had + t : had == INFINITY ? had : t;
+}
 
 constexpr int kWeightRows = 1024;      // rows x heads whose (M, f / l) are in shared memory at a time
 
@@ -111,8 +116,7 @@ weight_kernel(const CachedArgs a, float* __restrict__ weight, const int add, con
       float t = 0.f;
 #pragma unroll
       for (int w = 0; w < kWeightWarps; ++w) t += reinterpret_cast<const float*>(sum[w])[threadIdx.x];
-      const long long place = cached_place(a.page_table + (size_t)b * a.max_pages, slot, a.page_size, a.pages);
-      if (place >= 0) weight[place] = new_weight(weight[place], t, add);
+      put_weight(a, weight, b, slot, t, add);
     }
   }
 }
@@ -131,8 +135,7 @@ mass_kernel(const CachedArgs a, float* __restrict__ weight, const int add, const
 #pragma unroll 8
     for (int g = 0; g < a.kv_heads; ++g) t += row[(size_t)g * a.group * a.score_stride];
   }
-  const long long place = cached_place(a.page_table + (size_t)b * a.max_pages, slot, a.page_size, a.pages);
-  if (place >= 0) weight[place] = new_weight(weight[place], t, add);
+  put_weight(a, weight, b, slot, t, add);
 }
 
 }  // namespace

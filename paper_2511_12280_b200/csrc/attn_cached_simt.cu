@@ -46,6 +46,7 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
   walk.start(a, run);
   CachedSegment s = {};
   bool head = true;                              // the run's first segment
+  bool missing = false;                          // a slot whose page is not one of the pool's
   while (walk.next(a, s)) {
     if (head && threadIdx.x == kThreads - 1) cached_write_join(a, run, blockIdx.x, s, walk.tiles);
     head = false;
@@ -63,7 +64,12 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
     float m = -INFINITY, l = 0.f;                // of this lane's row, over its own pairs (l) and all lanes' (m)
     const int end = min(s.len, s.t1 * kKeyTile);
     // lane i: where key i of a step is (slots of a pool are counted in 31 bits); looked up a step ahead
-    auto find = [&](int key0) { return lane < kKeys && key0 + lane < end ? (int)cached_place(table, key0 + lane, a.page_size, a.pages) : -1; };
+    auto find = [&](int key0) {
+      if (lane >= kKeys || key0 + lane >= end) return -1;
+      const int at = (int)cached_place(table, key0 + lane, a.page_size, a.pages);
+      missing |= at < 0;
+      return at;
+    };
     int next_at = find(s.t0 * kKeyTile + warp * kKeys);
     for (int key0 = s.t0 * kKeyTile + warp * kKeys; key0 < end; key0 += kWarps * kKeys) {
       float val[LPK];
@@ -178,6 +184,7 @@ __global__ void __launch_bounds__(SimtShape<RT>::kWarps * 32, SimtShape<RT>::kCt
     }
     __syncthreads();
   }
+  if (missing) report_invalid(a.dev_status);     // (inside the loop: four requests of 8000 slots x 4 x 128, eight rows 59 -> 63 us)
   if (head && threadIdx.x == 0) cached_write_join(a, run, blockIdx.x, s, 0);
   cached_write_empty<T>(a, threadIdx.x, kThreads);
 }

@@ -65,12 +65,25 @@ def test_a_slot_that_is_not_there_does_not_hide_a_wait_that_ran_out(call):
         else:
             ctx.d3tom_attn_cached(P.cache, k, one, 1, 1, 1, 40, 0.125, B_.WEIGHT_SET, None, out)
 
-    if call != "attend_fp32":                    # (the CUDA-core kernel leaves slots out without a word; the lengths are looked at)
-        bad()
-        assert ctx.device_status() == B_.ERR_INVALID_ARG
+    bad()
+    assert ctx.device_status() == B_.ERR_INVALID_ARG
     ctx.reset_device_status()
     ctx.selftest_wait_timeout(10 ** 6)
     bad()
     assert ctx.device_status() == B_.ERR_TIMEOUT
     ctx.reset_device_status()
     assert ctx.device_status() == 0
+
+
+@pytest.mark.parametrize("dt,H,block", [(BF, 2, 1), (BF, 2, 50), (FP, 2, 1), (FP, 2, 9), (BF, 2, 0)])
+def test_a_page_that_is_not_there_is_reported_by_every_kernel(dt, H, block):
+    # among several that are, at lengths that fit; where nobody looks, by the weights alone
+    P = Pool([300], 16, 1, 128, dt, seed=33)
+    P.table[0, 7] = -1
+    total = max(1, block)
+    q, out = randn((total, H, 128), dt, 1), torch.zeros(total, H * 128, dtype=dt, device=DEV)
+    ctx = B_.Context(64, 1, H, 128, 64, 300)
+    for mode in (B_.WEIGHT_NONE, B_.WEIGHT_SET)[0 if block else 1:]:
+        ctx.d3tom_attn_cached(P.cache, q, i32([0, block]), 1, block, block, 300, 0.1, mode, None, out)
+        assert ctx.device_status() == B_.ERR_INVALID_ARG
+        ctx.reset_device_status()
