@@ -306,7 +306,7 @@ def _run_attn(st):
     if own:
         from paper_2511_12280_b200 import binding as B_
         mode = {"none": B_.WEIGHT_NONE, "add": B_.WEIGHT_ADD, "set": B_.WEIGHT_SET}[case["weight"]]
-        st["ctx"].d3tom_attn_cached(st["cache"], st["q"], st["cu_rows"], case["batch"], st["total"], case["rows"], st["L"], scale,
+        st["ctx"].d3tom_attn_cached(st["cache"], st["q"], st["cu_rows"], case["batch"], st["total"], max(st["rows"]), st["L"], scale,
                                     mode, st["row_weight"], st["out"])
         return st["out"][: st["total"]], st["w_all"][:n]
     B, H, kv, dh, L, N = case["batch"], case["heads"], case["kv_heads"], case["dh"], st["L"], case["rows"]
