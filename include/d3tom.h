@@ -373,7 +373,8 @@ int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache,
  * D3TOM_WEIGHT_SET stores that too.  Sums run in a fixed order: results are run-to-run identical.
  *  q           [total_rows, H, dh]; rows [cu_rows[b], cu_rows[b+1]) belong to request b; rows behind cu_rows[B] are
  *              neither read nor written
- *  max_rows    host: >= every request's rows;  max_length  host: >= every length[b] (smaller values cost time or cut)
+ *  max_rows    host: the most rows a request has, not more than total_rows (D3TOM_ERR_INVALID_ARG); a smaller number costs time
+ *  max_length  host: >= every length[b]; slots behind a smaller number are left out
  *  row_weight  [total_rows] fp32 or NULL (all 1)
  *  out         [total_rows, H*dh], not over q; rows of a request without slots are zero
  * Requests may share pages when they are only read; with a mode that writes weights no two requests of a call may.
