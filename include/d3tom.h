@@ -339,9 +339,9 @@ typedef struct {
 /* q_out, k_out = the rows of q and k rotated by their positions; inverse != 0 rotates back (the same call takes the
  * gradient of a rotation's output to its input).  q [rows, H, dh], k [rows, kv_heads, dh] or NULL (with k_out NULL);
  * positions [rows, axes] int32, any value.  q_out may be q and k_out may be k; otherwise the buffers must not overlap.
- * Angles are exact to 2^-32 of a turn at every position; cosine and sine are rounded to fp32, the result once to the
- * storage type.  dh must be a multiple of 4 (fp32) or 8 (bf16), here and in d3tom_cache_append.  All row buffers must be
- * 16-byte aligned. */
+ * Angles are within 2^-32 of a turn at every position (2^-28 for a theta below 10^4); cosine and sine are within two units
+ * of their last fp32 digit, and the result is rounded once to the storage type.  dh must be a multiple of 4 (fp32) or
+ * 8 (bf16), here and in d3tom_cache_append.  All row buffers must be 16-byte aligned. */
 int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
                const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
                d3tom_stream stream);

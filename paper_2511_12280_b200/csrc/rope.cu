@@ -1,9 +1,9 @@
 // Rotary positions (d3tom_rope) and the rows that go into a cache in pages (d3tom_cache_append).
 //
 // A pair (a, b) of a head becomes (a cos t - b sin t, a sin t + b cos t), t = position * theta^-e.  A position step is held as a
-// 64-bit fraction of a turn, so position * step is an integer product that wraps around where the angle does: its upper 32
-// bits are the angle to 2^-32 of a turn at every position (in fp32 the product itself would be off by radians from a million on),
-// and sincospif needs no range reduction.  The angles of a row are shared by its heads: a warp computes them once.  Bound: HBM (every
+// 64-bit fraction of a turn, so position * step is an integer product that wraps around where the angle does, and what it is off by
+// at any position is the table's error times the position (in fp32 the product itself would be off by radians from a million on);
+// sincospif needs no range reduction.  The angles of a row are shared by its heads: a warp computes them once.  Bound: HBM (every
 // row is read and written once); with few rows, latency.
 #include "common.cuh"
 
@@ -30,8 +30,15 @@ __device__ __forceinline__ void row_angles(const RotateArgs& a, const RopeTable&
     c[j] = 1.f; s[j] = 0.f;
     if (pr < t.pairs) {
       const long long pos = a.positions[(size_t)row * t.axes + axis[pr]];
-      const int32_t part = (int32_t)(((unsigned long long)pos * turn[pr]) >> 32);    // in 2^-32 of a turn, -1/2 .. 1/2
-      sincospif((float)part * 4.656612873077392578125e-10f, &s[j], &c[j]);           // half turns: part * 2^-31
+      // in 2^-64 of a turn, -1/2 .. 1/2: the 25 upper bits, which fp32 holds, and the small rest d (below 2e-7 radians, taken to 2^-48
+      // of a turn) by cos(x + d) = cos x - d sin x, sin(x + d) = sin x + d cos x
+      const unsigned long long part = (unsigned long long)pos * turn[pr];
+      const int32_t upper = (int32_t)(part >> 32) & ~127;
+      const float d = (float)(int32_t)((part >> 16) & 0x7fffffu) * (3.14159265358979f * 0x1p-47f);
+      sincospif((float)upper * 0x1p-31f, &s[j], &c[j]);                              // in half turns
+      const float c0 = c[j];
+      c[j] = fmaf(-s[j], d, c0);
+      s[j] = fmaf(c0, d, s[j]);
       if (a.inverse) s[j] = -s[j];
     }
   }

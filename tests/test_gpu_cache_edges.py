@@ -11,6 +11,30 @@ from test_gpu_cache import BF, DEV, FP, Pool, check_attention, cu, f64, i32, ran
 pytestmark = pytest.mark.gpu
 
 
+# ------------------------------------------------------------------ angles
+@pytest.mark.parametrize("theta,turns", [(1e4, 2.0 ** -32), (1e6, 2.0 ** -32), (1.5, 2.0 ** -28)])
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_angles_of_far_positions(theta, turns, neighbours):
+    # the pair (1, 0) becomes (cos, sin), which are small themselves near quarter and half turns: there the angle's own error is seen.
+    # Bound: the angle, 2 units of the last digit (sincospif 1, the rest of the angle 1/2, both at most 2^-23 of the value)
+    rows, H, dh = 2048, 1, 128
+    pos = np.random.default_rng(7).integers(-2 ** 31, 2 ** 31, (rows, 1))
+    pos[:4, 0] = [0, 1, 2 ** 31 - 1, -2 ** 31]
+    x = torch.zeros(rows, H, dh, device=DEV)
+    x[..., 0::2] = 1.0
+    if not neighbours:
+        x = torch.cat([torch.ones(rows, H, dh // 2, device=DEV), torch.zeros(rows, H, dh // 2, device=DEV)], dim=-1).contiguous()
+    spec = B_.RopeSpec([64], theta, B_.PAIR_NEIGHBOURS if neighbours else B_.PAIR_HALVES)
+    out = torch.empty_like(x)
+    B_.Context(rows, 1, H, dh, 1, 1).d3tom_rope(spec, x, None, i32(pos), rows, 0, out, None)
+    y = f64(out)[:, 0]
+    c, s = (y[:, 0::2], y[:, 1::2]) if neighbours else (y[:, : dh // 2], y[:, dh // 2 :])
+    ang = co.rope_angles(pos, [64], theta, False)
+    assert (np.abs(np.sin(ang)) < 0.01).sum() > 500 and (np.abs(np.cos(ang)) < 0.01).sum() > 500
+    for got, want in ((c, np.cos(ang)), (s, np.sin(ang))):
+        assert (np.abs(got - want) <= 2 * np.pi * turns + 2 * 2.0 ** -23 * np.abs(want)).all()
+
+
 # ------------------------------------------------------------------ protected slots
 # columns per key head: few, whose scores go out, and many, whose weights come from a second pass over the keys
 @pytest.mark.parametrize("dt,H,kv,dh,block", [(BF, 4, 2, 128, 1), (BF, 4, 1, 128, 16), (BF, 4, 2, 64, 3), (BF, 8, 2, 64, 9), (FP, 4, 2, 64, 3)])
