@@ -306,7 +306,8 @@ int d3tom_merge_kv(d3tom_ctx* ctx, d3tom_dtype dt, d3tom_agg mode,
  * model; positions, pages and eviction follow the formulas given here.
  *
  * Slot j of request b is row j % page_size of page page_table[b][j / page_size].  A request has length[b] slots, in no
- * order that attention depends on: keys are stored with their positions already in them. */
+ * order that attention depends on: keys are stored with their positions already in them.  Where a call has no rows, pointers
+ * to rows may be NULL. */
 typedef struct {
   void* k;                      /* [pages, page_size, kv_heads, dh] storage type */
   void* v;                      /* [pages, page_size, kv_heads, dh] storage type */

@@ -486,7 +486,7 @@ static int make_rope_table(const d3tom_rope_spec* sp, int dh, RopeTable* t) {
 static int rope_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
                      const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
                      cudaStream_t s) {
-  if (ctx == nullptr || spec == nullptr || q == nullptr || q_out == nullptr || positions == nullptr ||
+  if (ctx == nullptr || spec == nullptr || (rows > 0 && (q == nullptr || q_out == nullptr || positions == nullptr)) ||
       (k == nullptr) != (k_out == nullptr) || rows < 0 || (k != nullptr && kv_heads <= 0))
     return D3TOM_ERR_INVALID_ARG;
   if (!dtype_ok(dt)) return D3TOM_ERR_UNSUPPORTED;
@@ -533,8 +533,8 @@ static int append_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache,
                        cudaStream_t s) {
   int st = check_cache(ctx, dt, cache, B);
   if (st != D3TOM_OK) return st;
-  if (k == nullptr || v == nullptr || cu_rows == nullptr || total_rows < 0 || (q == nullptr) != (q_out == nullptr) ||
-      (spec != nullptr && positions == nullptr) || (tokens != nullptr && cache->token == nullptr) ||
+  if ((total_rows > 0 && (k == nullptr || v == nullptr || (spec != nullptr && positions == nullptr))) || cu_rows == nullptr ||
+      total_rows < 0 || (q == nullptr) != (q_out == nullptr) || (tokens != nullptr && cache->token == nullptr) ||
       (first_weight != nullptr && cache->weight == nullptr))
     return D3TOM_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return D3TOM_ERR_INVALID_ARG;
@@ -568,7 +568,7 @@ static int attn_cached_impl(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* c
                             d3tom_weight_mode mode, const float* row_weight, void* out, cudaStream_t s) {
   int st = check_cache(ctx, dt, cache, B);
   if (st != D3TOM_OK) return st;
-  if (q == nullptr || out == nullptr || cu_rows == nullptr || total_rows < 0 || max_rows < 0 || max_rows > total_rows ||
+  if ((total_rows > 0 && (q == nullptr || out == nullptr)) || cu_rows == nullptr || total_rows < 0 || max_rows < 0 || max_rows > total_rows ||
       max_length < 0 || !(softmax_scale > 0.f) || !isfinite(softmax_scale) || !aligned16(q) || !aligned16(out))
     return D3TOM_ERR_INVALID_ARG;
   if (mode != D3TOM_WEIGHT_NONE && mode != D3TOM_WEIGHT_ADD && mode != D3TOM_WEIGHT_SET) return D3TOM_ERR_INVALID_ARG;

@@ -111,3 +111,24 @@ def test_a_page_that_is_not_there_is_reported_by_every_kernel(dt, H, block):
         ctx.d3tom_attn_cached(P.cache, q, i32([0, block]), 1, block, block, 300, 0.1, mode, None, out)
         assert ctx.device_status() == B_.ERR_INVALID_ARG
         ctx.reset_device_status()
+
+
+# ------------------------------------------------------------------ calls without rows
+@pytest.mark.parametrize("dt", [BF, FP])
+def test_steps_in_which_nobody_has_rows(dt):
+    # tensors of no rows have no address
+    C = PagedCache(2, 4, 2, 64, dt, pages=4, page_size=8, max_rows=16, max_length=16, max_scored_rows=4)
+    k = randn((5, 2, 64), dt, 1)
+    C.append([2, 3], k, k, i32(np.arange(5)), first_weight=torch.tensor([1.0, float("inf"), 2.0, 3.0, 4.0], device=DEV))
+    q, kv, none = torch.empty(0, 4, 64, dtype=dt, device=DEV), torch.empty(0, 2, 64, dtype=dt, device=DEV), i32([])
+    before = [t.clone() for t in (C.k, C.v, C.weight, C.token)]
+    spec = B_.RopeSpec([8, 8])
+    C.append([0, 0], kv, kv, none, q=q, q_out=torch.empty_like(q), spec=spec, positions=none.view(0, 2), first_weight=torch.empty(0, device=DEV))
+    C.attend([0, 0], q, torch.empty(0, 256, dtype=dt, device=DEV))
+    C.ctx.d3tom_rope(spec, q, kv, none.view(0, 2), 0, 2, torch.empty_like(q), torch.empty_like(kv))
+    assert C.lengths_h == [2, 3] and C.ctx.device_status() == 0
+    for x, y in zip((C.k, C.v, C.weight, C.token), before):
+        assert torch.equal(x, y)
+    C.attend([0, 0], q, torch.empty(0, 256, dtype=dt, device=DEV), B_.WEIGHT_SET, row_weight=torch.empty(0, device=DEV))
+    at = [torch.as_tensor(co.places(C.table_h[b], C.lengths_h[b], 8), device=DEV) for b in range(2)]
+    assert C.weight.view(-1)[at[0]].tolist() == [0.0, float("inf")] and C.weight.view(-1)[at[1]].tolist() == [0.0] * 3
