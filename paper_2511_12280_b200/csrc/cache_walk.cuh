@@ -163,17 +163,32 @@ __device__ __forceinline__ void cached_write_join(const CachedArgs& a, const Cac
 }
 
 // What no run has: zeros for the rows of requests without slots, and the word on lengths that do not fit.  `threads` threads of
-// every CTA, this one the `tid`-th of them.
+// every CTA, this one the `tid`-th of them: whole warps.  All CTAs share such a request's rows, 16 bytes at a time (8 where rows are odd
+// multiples of that).  (By one warp of one CTA, a number at a time / so, us: 40 rows x 32 heads x 128 of an empty request 24.4 / 2.9, seven
+// blocks of 32 rows over 1088 slots beside one over none 34.8 / 29.6.)
 template <typename T>
 __device__ __forceinline__ void cached_write_empty(const CachedArgs& a, int tid, int threads) {
-  for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
-    const CachedRequest r = cached_request(a, b);
-    const int raw = a.length[b];
-    if (tid == 0 && (raw < 0 || raw > a.cap)) report_invalid(a.dev_status);
-    if (r.len > 0) continue;
-    T* out = static_cast<T*>(a.out) + (size_t)r.lo * a.H * a.dh;
-    const size_t count = (size_t)r.n * a.H * a.dh;
-    for (size_t i = tid; i < count; i += threads) out[i] = Storage<T>::from_float(0.f);
+  const int lane = threadIdx.x & 31, row_bytes = a.H * a.dh * (int)sizeof(T);
+  auto zero = [&](auto unit, const CachedRequest& r) {
+    using U = decltype(unit);
+    U* out = reinterpret_cast<U*>(static_cast<uint8_t*>(a.out) + (size_t)r.lo * row_bytes);
+    const size_t count = (size_t)r.n * (row_bytes / sizeof(U));
+    for (size_t i = (size_t)blockIdx.x * threads + tid; i < count; i += (size_t)gridDim.x * threads) out[i] = U{};
+  };
+  for (int b0 = 0; b0 < a.B; b0 += 32) {
+    const int b = b0 + lane;
+    bool empty = false;
+    if (b < a.B) {
+      const CachedRequest r = cached_request(a, b);
+      empty = r.len == 0 && r.n > 0;
+      const int raw = a.length[b];
+      if (blockIdx.x == 0 && (raw < 0 || raw > a.cap)) report_invalid(a.dev_status);
+    }
+    for (unsigned left = __ballot_sync(0xffffffffu, empty); left != 0u; left &= left - 1u) {
+      const CachedRequest r = cached_request(a, b0 + __ffs(left) - 1);
+      if (row_bytes % 16 == 0) zero(uint4(), r);
+      else zero(uint2(), r);
+    }
   }
 }
 

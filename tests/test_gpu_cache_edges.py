@@ -132,3 +132,16 @@ def test_steps_in_which_nobody_has_rows(dt):
     C.attend([0, 0], q, torch.empty(0, 256, dtype=dt, device=DEV), B_.WEIGHT_SET, row_weight=torch.empty(0, device=DEV))
     at = [torch.as_tensor(co.places(C.table_h[b], C.lengths_h[b], 8), device=DEV) for b in range(2)]
     assert C.weight.view(-1)[at[0]].tolist() == [0.0, float("inf")] and C.weight.view(-1)[at[1]].tolist() == [0.0] * 3
+
+
+# ------------------------------------------------------------------ requests without slots
+@pytest.mark.parametrize("dt,H,dh,reference", [(BF, 32, 128, False), (BF, 6, 64, False), (BF, 3, 12, True), (FP, 5, 36, False), (FP, 1, 4, False)])
+def test_rows_of_requests_without_slots_are_zero(dt, H, dh, reference):
+    # more of them than a warp has lanes, some of one row; what lies behind the last row is left alone
+    lens = [0 if b % 3 else 20 for b in range(70)]
+    lens[69] = 0
+    rows = [b % 4 if b < 69 else 40 for b in range(70)]
+    out, _ = check_attention(Pool(lens, 8, 1, dh, dt, seed=34), H, rows, pad=3, reference=reference)
+    for b, n in enumerate(lens):
+        if n == 0:
+            assert not out[cu(rows)[b] : cu(rows)[b + 1]].any()
