@@ -145,3 +145,79 @@ def test_rows_of_requests_without_slots_are_zero(dt, H, dh, reference):
     for b, n in enumerate(lens):
         if n == 0:
             assert not out[cu(rows)[b] : cu(rows)[b + 1]].any()
+
+
+# ------------------------------------------------------------------ tile widths
+@pytest.mark.parametrize("mode", [B_.WEIGHT_NONE, B_.WEIGHT_ADD, B_.WEIGHT_SET])
+@pytest.mark.parametrize("H,kv,dh,block", [(3, 1, 64, 11), (2, 2, 64, 33), (8, 2, 64, 16), (5, 5, 64, 64), (3, 1, 128, 11), (4, 4, 128, 64), (2, 1, 128, 20)])
+def test_blocks_of_33_to_64_columns(H, kv, dh, block, mode):
+    rows = [block, 0, 1, block - 1, block, 2, 0, block]
+    P = Pool([0, 1, 127, 128, 129, 640, 33, 1300], 8, kv, dh, BF, seed=35)
+    check_attention(P, H, rows, mode, np.random.default_rng(2).uniform(-1, 2, sum(rows)))
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("block", [4, 8, 12, 16, 25, 32, 45])
+def test_scores_that_grow_along_the_cache_at_every_tile_width(dh, block):
+    # 16 .. 180 columns: the running maximum outgrows its reference from tile to tile in one request and falls in the other
+    P = Pool([1500, 700], 16, 1, dh, BF, seed=36)
+    for b in range(2):
+        idx = torch.as_tensor(P.at[b], device=DEV)
+        ramp = torch.linspace(0.01, 6.0, 1500, device=DEV) if b == 0 else torch.linspace(5.0, 0.0, 700, device=DEV)
+        k = P.flat()[0]
+        k[idx] = (k[idx].float() * ramp[:, None, None]).to(BF)
+    check_attention(P, 4, [block, 3], B_.WEIGHT_SET, q=randn((block + 5, 4, dh), BF, 3, 3.0))
+
+
+@pytest.mark.parametrize("dt,dh", [(BF, 128), (BF, 64), (FP, 64)])
+@pytest.mark.parametrize("said", [0, 1, 9])
+def test_more_rows_than_the_call_was_told(dt, dh, said):
+    # max_rows chooses a tile's width, and no result but the order of sums
+    lens, rows = [300, 150], [40, 7]
+    P = Pool(lens, 16, 2, dh, dt, seed=37)
+    q, ctx = randn((47, 4, dh), dt, 1), B_.Context(64, 2, 4, dh, 47, 300)
+    res = []
+    for most in (40, said):
+        w = torch.zeros_like(P.weight)
+        out = torch.zeros(47, 4 * dh, dtype=dt, device=DEV)
+        cache = B_.Cache(P.k, P.v, w, P.token, P.table, P.length)
+        ctx.d3tom_attn_cached(cache, q, i32(cu(rows)), 2, 47, most, 300, dh ** -0.5, B_.WEIGHT_SET, None, out)
+        res.append((f64(out), f64(w)))
+    # bf16: two roundings of P and one of the result on either side, of sums of |v| p up to 4
+    assert np.abs(res[0][0] - res[1][0]).max() <= (4 * 4 * 2.0 ** -8 if dt == BF else 1e-4)
+    assert np.abs(res[0][1] - res[1][1]).max() <= 1e-3 * np.abs(res[0][1]).max() and ctx.device_status() == 0
+
+
+# ------------------------------------------------------------------ slots that are not there
+@pytest.mark.parametrize("dt,H,kv,dh,block", [(BF, 2, 2, 128, 1), (BF, 2, 2, 128, 32), (BF, 2, 2, 128, 40), (BF, 4, 1, 128, 30), (BF, 2, 2, 64, 20), (BF, 2, 1, 64, 40),
+                                              (FP, 4, 2, 64, 1), (FP, 4, 2, 64, 9)])
+@pytest.mark.parametrize("mode", [B_.WEIGHT_ADD, B_.WEIGHT_SET])
+def test_weights_of_slots_that_are_not_there_keep_every_bit(dt, H, kv, dh, block, mode):
+    P = Pool([700, 90], 16, kv, dh, dt, seed=38)
+    P.table[0, 3] = P.pages
+    P.length[1] = 10 ** 6                        # behind max_length: 90 slots are looked at
+    P.table[1, 6:] = -1
+    gone, whole = P.at[0][48:64], P.at[0]
+    there = [np.concatenate([whole[:48], whole[64:]]), P.at[1]]
+    q, rows = randn((block + 1, H, dh), dt, 1), [block, 1]
+    before = P.copy()
+    out = torch.zeros(block + 1, H * dh, dtype=dt, device=DEV)
+    ctx = B_.Context(64, 2, H, dh, block + 1, 700)
+    ctx.d3tom_attn_cached(P.cache, q, i32(cu(rows)), 2, block + 1, block, 700, dh ** -0.5, mode, None, out)
+    assert ctx.device_status() == B_.ERR_INVALID_ARG
+    k1, v1, w1, t1 = P.flat()
+    for b in range(2):
+        lo, hi, idx = cu(rows)[b], cu(rows)[b + 1], torch.as_tensor(there[b], device=DEV)
+        if b == 1:                               # its table ends with the page of slot 95: the slots behind its 90 are anything
+            continue
+        o, p, mag, _ = co.attend(f64(q[lo:hi]), f64(k1[idx]), f64(v1[idx]), dh ** -0.5)
+        assert (np.abs(f64(out[lo:hi]).reshape(o.shape) - o) <= 2.0 ** -7 * mag + 1e-4).all()
+        want = p.sum(axis=(0, 1)) + (f64(before[2])[there[b]] if mode == B_.WEIGHT_ADD else 0.0)
+        assert (np.abs(f64(w1)[there[b]] - want) <= 5e-4 * want).all()
+    touched = np.zeros(len(w1), bool)
+    touched[there[0]] = True
+    touched[co.places(P.table_h[1], 96, 16)] = True
+    assert not touched[gone].any()
+    rest = torch.as_tensor(~touched, device=DEV)
+    assert torch.equal(w1[rest], before[2][rest]) and torch.equal(t1, before[3])
+    assert torch.equal(k1.nan_to_num(99), before[0].nan_to_num(99)) and torch.equal(v1.nan_to_num(99), before[1].nan_to_num(99))
