@@ -221,3 +221,67 @@ def test_weights_of_slots_that_are_not_there_keep_every_bit(dt, H, kv, dh, block
     rest = torch.as_tensor(~touched, device=DEV)
     assert torch.equal(w1[rest], before[2][rest]) and torch.equal(t1, before[3])
     assert torch.equal(k1.nan_to_num(99), before[0].nan_to_num(99)) and torch.equal(v1.nan_to_num(99), before[1].nan_to_num(99))
+
+
+# ------------------------------------------------------------------ a merged prefix, cached and decoded against
+@pytest.mark.parametrize("dt,H,dh,page", [(BF, 4, 128, 16), (BF, 4, 64, 24), (FP, 3, 32, 5)])
+def test_a_merged_prefix_goes_into_the_pages_and_is_attended_to(dt, H, dh, page):
+    """d3tom_merge_kv's shortened K and V with their source rows as token numbers -> PagedCache -> a response block with weights ->
+    eviction that keeps the prompt; against fp64 on the merged rows that the merge itself is checked to give."""
+    n_vis, n_prompt, keep = [150, 61], [9, 4], [40, 20]
+    lens, out_lens = [v + p for v, p in zip(n_vis, n_prompt)], [k + p for k, p in zip(keep, n_prompt)]
+    D, total, total_out = H * dh, sum(lens), sum(out_lens)
+    rng = np.random.default_rng(5)
+    kept = [np.sort(rng.choice(v, k, replace=False)).astype(np.int32) for v, k in zip(n_vis, keep)]
+    k, v = randn((total, D), dt, 1), randn((total, D), dt, 2)
+    k_out, v_out = torch.empty(total_out, D, dtype=dt, device=DEV), torch.empty(total_out, D, dtype=dt, device=DEV)
+    assign, count, src = i32(np.zeros(sum(n_vis))), i32(np.zeros(sum(keep))), i32(np.zeros(total_out))
+    merge = B_.Context(total, 2, H, dh, 1, max(n_vis))
+    merge.d3tom_merge_kv(B_.AGG_MEAN, k, v, i32(cu(lens)), i32(n_vis), i32(cu(n_vis)), i32(np.concatenate(kept)), i32(cu(keep)), 2, D, total,
+                         total_out, max(n_vis), max(keep), k_out, v_out, i32(cu(out_lens)), assign, count, src)
+    # prompt rows are copies, and the merge says where every row came from
+    src_h = src.cpu().numpy()
+    for b in range(2):
+        rows_b = np.concatenate([kept[b], np.arange(n_vis[b], lens[b])]) + cu(lens)[b]
+        assert np.array_equal(src_h[cu(out_lens)[b] : cu(out_lens)[b + 1]], rows_b)
+        prompt = slice(cu(out_lens)[b] + keep[b], cu(out_lens)[b + 1])
+        assert torch.equal(k_out[prompt], k[torch.as_tensor(src_h[prompt], device=DEV).long()])
+    block = [5, 3]
+    C = PagedCache(2, H, H, dh, dt, pages=sum(-(-(n + r) // page) for n, r in zip(out_lens, block)), page_size=page, max_rows=total_out,
+                   max_length=max(out_lens) + 5, max_scored_rows=8)
+    is_prompt = np.concatenate([np.arange(n) >= q for n, q in zip(out_lens, keep)])
+    first = torch.where(torch.as_tensor(is_prompt, device=DEV), float("inf"), 0.0).to(FP)
+    C.append(out_lens, k_out, v_out, src, first_weight=first)
+    q, kb, vb = randn((8, H, dh), dt, 3), randn((8, H, dh), dt, 4), randn((8, H, dh), dt, 5)
+    out = torch.empty(8, D, dtype=dt, device=DEV)
+    C.append(block, kb, vb, i32(np.arange(8) + 100000))
+    C.attend(block, q, out, B_.WEIGHT_SET)
+    mass = []
+    for b in range(2):
+        lo, hi, n = cu(block)[b], cu(block)[b + 1], out_lens[b]
+        at = torch.as_tensor(co.places(C.table_h[b], n + block[b], page), device=DEV)
+        part = slice(cu(out_lens)[b], cu(out_lens)[b + 1])
+        keys, values = (torch.cat([x[part].view(-1, H, dh), y[lo:hi]]) for x, y in ((k_out, kb), (v_out, vb)))
+        assert torch.equal(C.k.view(-1, H, dh)[at], keys) and torch.equal(C.v.view(-1, H, dh)[at], values)
+        assert C.token.view(-1)[at].tolist() == src_h[part].tolist() + list(range(100000 + lo, 100000 + hi))
+        o, p, mag, _ = co.attend(f64(q[lo:hi]), f64(keys), f64(values), dh ** -0.5)
+        # P and the result rounded (bf16), sums of dh products and of up to 54 terms (fp32)
+        assert (np.abs(f64(out[lo:hi]).reshape(o.shape) - o) <= (2.0 ** -7 if dt == BF else 0) * mag + 5e-4 * mag).all()
+        m = p.sum(axis=(0, 1))
+        got = f64(C.weight.view(-1)[at])
+        assert np.isinf(got[keep[b] : n]).all() and (np.abs(np.delete(got - m, np.s_[keep[b] : n])) <= 5e-4 * np.delete(m, np.s_[keep[b] : n])).all()
+        mass.append(got[:n])
+    C.drop_last(block)
+    budget = [12, 10]
+    want = [[src_h[cu(out_lens)[b] + j] for j in range(out_lens[b])] for b in range(2)]
+    for b in range(2):
+        n, moves = co.evict(mass[b], None, budget[b])
+        for s, d in moves:
+            want[b][d] = want[b][s]
+        want[b] = want[b][:n]
+    C.evict(budget)
+    for b in range(2):
+        at = torch.as_tensor(co.places(C.table_h[b], C.lengths_h[b], page), device=DEV)
+        assert C.token.view(-1)[at].tolist() == want[b]
+        assert set(src_h[is_prompt & (np.repeat([0, 1], out_lens) == b)].tolist()) <= set(want[b])
+    assert C.ctx.device_status() == 0 and merge.device_status() == 0
