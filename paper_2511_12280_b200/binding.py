@@ -157,12 +157,6 @@ def _ptr(t: Optional[torch.Tensor]):
     return t.data_ptr()              # (the signatures convert it: an object per argument is a third of a call's host time)
 
 
-def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
-
-
 def _i32(t: Optional[torch.Tensor], least: int):
     """Pointer of an int32 array of at least `least` numbers."""
     if t is not None and (t.dtype != torch.int32 or t.numel() < least):
@@ -253,7 +247,7 @@ def d3tom_attn_importance_static(heads, head_dim, q, k, v, cu_seqlens, n_visual,
                                                _ptr(n_visual), _ptr(decider_pos), _ptr(cu_deciders), B, total_tokens,
                                                max_seqlen, max_visual, n_deciders_total, softmax_scale,
                                                _ptr(attn_out), _ptr(importance), _ptr(cu_vis),
-                                               _ptr(device_status_out), _stream(stream)),
+                                               _ptr(device_status_out), _raw_stream(stream, torch.cuda.current_device())),
            "d3tom_attn_importance_static")
 
 
@@ -296,7 +290,7 @@ class Context:
 
     def selftest_wait_timeout(self, limit_ns: int, stream=None):
         """Enqueues the one-block kernel whose wait cannot end; afterwards device_status() is ERR_TIMEOUT."""
-        _check(load().d3tom_selftest_wait_timeout(self._h, int(limit_ns), _stream(stream)), "d3tom_selftest_wait_timeout")
+        _check(load().d3tom_selftest_wait_timeout(self._h, int(limit_ns), _raw_stream(stream, self.device)), "d3tom_selftest_wait_timeout")
 
     # -------------------------------------------------------------- the four calls (+ projection)
     def d3tom_attn_importance(self, q, k, v, cu_seqlens, n_visual, decider_pos, cu_deciders, B, total_tokens,
@@ -305,11 +299,11 @@ class Context:
         _check(load().d3tom_attn_importance(self._h, _dt(q), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens),
                                             _ptr(n_visual), _ptr(decider_pos), _ptr(cu_deciders), B, total_tokens,
                                             max_seqlen, max_visual, n_deciders_total, softmax_scale, _ptr(attn_out),
-                                            _ptr(importance), _ptr(cu_vis), _stream(stream)), "d3tom_attn_importance")
+                                            _ptr(importance), _ptr(cu_vis), _raw_stream(stream, self.device)), "d3tom_attn_importance")
 
     def d3tom_select(self, importance, cu_vis, keep_count, cu_kept, B, max_visual, kept_idx, keep_mask, stream=None):
         _check(load().d3tom_select(self._h, _ptr(importance), _ptr(cu_vis), _ptr(keep_count), _ptr(cu_kept), B,
-                                   max_visual, _ptr(kept_idx), _ptr(keep_mask), _stream(stream)), "d3tom_select")
+                                   max_visual, _ptr(kept_idx), _ptr(keep_mask), _raw_stream(stream, self.device)), "d3tom_select")
 
     def d3tom_merge(self, mode, hidden, cu_seqlens, n_visual, cu_vis, kept_idx, cu_kept, B, D, total_tokens,
                     total_out, max_visual, max_kept, hidden_out, cu_seqlens_out, assign, member_count, src_of_dst,
@@ -317,7 +311,7 @@ class Context:
         _check(load().d3tom_merge(self._h, _dt(hidden), mode, _ptr(hidden), _ptr(cu_seqlens), _ptr(n_visual),
                                   _ptr(cu_vis), _ptr(kept_idx), _ptr(cu_kept), B, D, total_tokens, total_out,
                                   max_visual, max_kept, _ptr(hidden_out), _ptr(cu_seqlens_out), _ptr(assign),
-                                  _ptr(member_count), _ptr(src_of_dst), _ptr(sim_debug), _stream(stream)),
+                                  _ptr(member_count), _ptr(src_of_dst), _ptr(sim_debug), _raw_stream(stream, self.device)),
                "d3tom_merge")
 
     def d3tom_merge_kv(self, mode, k_cache, v_cache, cu_seqlens, n_visual, cu_vis, kept_idx, cu_kept, B, D, total_tokens,
@@ -327,25 +321,25 @@ class Context:
                                      _ptr(n_visual), _ptr(cu_vis), _ptr(kept_idx), _ptr(cu_kept), B, D, total_tokens,
                                      total_out, max_visual, max_kept, _ptr(k_out), _ptr(v_out), _ptr(cu_seqlens_out),
                                      _ptr(assign), _ptr(member_count), _ptr(src_of_dst), _ptr(sim_debug),
-                                     _stream(stream)), "d3tom_merge_kv")
+                                     _raw_stream(stream, self.device)), "d3tom_merge_kv")
 
     def d3tom_attn_varlen(self, q, k, v, cu_seqlens, B, total_tokens, max_seqlen, softmax_scale, out, stream=None):
         _check(load().d3tom_attn_varlen(self._h, _dt(q), _ptr(q), _ptr(k), _ptr(v), _ptr(cu_seqlens), B,
-                                        total_tokens, max_seqlen, softmax_scale, _ptr(out), _stream(stream)),
+                                        total_tokens, max_seqlen, softmax_scale, _ptr(out), _raw_stream(stream, self.device)),
                "d3tom_attn_varlen")
 
     def d3tom_proj_qkv(self, x, w_qkv, total, D, q, k, v, stream=None):
         _check(load().d3tom_proj_qkv(self._h, _dt(x), _ptr(x), _ptr(w_qkv), total, D, _ptr(q), _ptr(k), _ptr(v),
-                                     _stream(stream)), "d3tom_proj_qkv")
+                                     _raw_stream(stream, self.device)), "d3tom_proj_qkv")
 
     def d3tom_linear(self, x, w, residual, rows, K, N, out, stream=None):
         _check(load().d3tom_linear(self._h, _dt(x), _ptr(x), _ptr(w), _ptr(residual) if residual is not None else None,
-                                   rows, K, N, _ptr(out), _stream(stream)), "d3tom_linear")
+                                   rows, K, N, _ptr(out), _raw_stream(stream, self.device)), "d3tom_linear")
 
     def d3tom_ffn(self, x, w_gate_up, w_down, residual, rows, D, m, act, out, stream=None):
         _check(load().d3tom_ffn(self._h, _dt(x), _ptr(x), _ptr(w_gate_up), _ptr(w_down),
                                 _ptr(residual) if residual is not None else None, rows, D, m, _ptr(act), _ptr(out),
-                                _stream(stream)), "d3tom_ffn")
+                                _raw_stream(stream, self.device)), "d3tom_ffn")
 
     # -------------------------------------------------------------- a K/V cache in pages
     # (numbers of rows that are beyond the context's limits are not asked for: the library refuses those calls itself)
