@@ -38,8 +38,8 @@
  *    context must not overlap on the GPU (use one context per stream).
  *  - Every function returns a status: D3TOM_OK (0) or a negative error.  No
  *    exceptions, no abort, nothing printed (unless the environment variable
- *    D3TOM_LOG is set to something other than 0: then d3tom_create and the four
- *    calls of the path write one line per call, sizes and status, to stderr).  Argument errors are detected on
+ *    D3TOM_LOG is set to something other than 0: then d3tom_create, the calls of
+ *    the path and those on a cache in pages write one line per call, sizes and status, to stderr).  Argument errors are detected on
  *    the host before anything is launched.  Problems only the device can see
  *    (a bounded wait that ran out) are recorded in a status word read by
  *    d3tom_device_status.
@@ -342,7 +342,8 @@ typedef struct {
  * positions [rows, axes] int32, any value.  q_out may be q and k_out may be k; otherwise the buffers must not overlap.
  * Angles are within 2^-32 of a turn at every position (2^-28 for a theta below 10^4); cosine and sine are within two units
  * of their last fp32 digit, and the result is rounded once to the storage type.  dh must be a multiple of 4 (fp32) or
- * 8 (bf16), here and in d3tom_cache_append.  All row buffers must be 16-byte aligned. */
+ * 8 (bf16), rows at most max_total_tokens and kv_heads at most heads (D3TOM_ERR_WORKSPACE), here and in
+ * d3tom_cache_append.  All row buffers must be 16-byte aligned. */
 int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, const void* q, const void* k,
                const int32_t* positions, int rows, int kv_heads, int inverse, void* q_out, void* k_out,
                d3tom_stream stream);
@@ -358,7 +359,7 @@ int d3tom_rope(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_rope_spec* spec, cons
  *             there: no mode of d3tom_attn_cached takes it away
  *  cu_rows    [B+1] int32, prefix sum of the new rows; total_rows == cu_rows[B] (host copy); rows behind cu_rows[B]
  *             are neither read nor written
- * Two rows of one call must not have the same slot.  A row whose slot does not exist is dropped (see d3tom_attn_cached).
+ * Two rows of one call must not have the same place in the pools.  A row whose slot does not exist is dropped (see d3tom_attn_cached).
  * Row buffers, cache->k and cache->v must be 16-byte aligned. */
 int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const d3tom_rope_spec* spec,
                        const void* q, const void* k, const void* v, const int32_t* positions, const int32_t* tokens,
@@ -378,7 +379,8 @@ int d3tom_cache_append(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache,
  *  max_length  host: >= every length[b]; slots behind a smaller number are left out
  *  row_weight  [total_rows] fp32 or NULL (all 1)
  *  out         [total_rows, H*dh], not over q; rows of a request without slots are zero
- * Requests may share pages when they are only read; with a mode that writes weights no two requests of a call may.
+ * Requests may share pages when they are only read; with a mode that writes weights no page may stand twice in the tables of
+ * a call's requests.
  * The weights need scratch of the context's decider scores: total_rows <= max_deciders and max_length <=
  * max_visual_per_request, D3TOM_ERR_WORKSPACE otherwise.  bf16 on the tensor-core path needs page_size % 8 == 0
  * (D3TOM_ERR_UNSUPPORTED otherwise).  q, out, cache->k and cache->v must be 16-byte aligned.
@@ -399,7 +401,7 @@ int d3tom_attn_cached(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, 
  *  protect_from  [B] int32 or NULL (no slot is protected); needs cache->token
  *  length_out    [B] int32; may be the array cache->length
  *  max_length    host: >= every length[b]
- * No two requests of a call may share a page that is moved into.  Scratch: B * (max_length + 1) words out of
+ * A page that is moved into must stand in the tables once.  Scratch: B * (max_length + 1) words out of
  * max_total_tokens * heads * dh, D3TOM_ERR_WORKSPACE beyond. */
 int d3tom_cache_evict(d3tom_ctx* ctx, d3tom_dtype dt, const d3tom_cache* cache, const int32_t* budget,
                       const int32_t* protect_from, int B, int max_length, int32_t* length_out, d3tom_stream stream);

@@ -3,8 +3,8 @@
 //
 // Join: with (O_i, M_i, l_i) of the segments of an item, M = max M_i, l = sum l_i 2^(M_i - M), O = sum O_i 2^(M_i - M) / l.
 // Weight of slot j: sum over the rows i and query heads h of f_i 2^(s_ihj c - M_ih) / l_ih, from the raw scores that the attention
-// kernel left (weight_kernel: HBM, 88 MB in 20 us; latency where they are few) or from what its second pass summed already (mass_kernel:
-// latency).  All in a fixed order.
+// kernel left (weight_kernel: 88 MB in 20 us, two thirds of what a copy gets, partly from L2; latency where they are few) or from what its
+// second pass summed already (mass_kernel: latency).  All in a fixed order.
 #include "cache_walk.cuh"
 #include "ptx.cuh"
 
@@ -59,7 +59,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_kernel(const CachedArgs 
   if (lane == 0 && a.lse != nullptr) a.lse[row] = make_float2(m, l);
 }
 
-// Mass `t` into the weight of a request's slot.  +inf, which keeps a slot from being evicted, stays when weights are set.
+// Mass `t` into the weight of a request's slot.  +inf, which keeps a slot from being evicted, stays when weights are set.  (Looked up and
+// read ahead of the sums, or between them, it holds back their loads: one block of 64 rows x 32 heads over 1216 slots 31.4 -> 33.4 us.)
 __device__ __forceinline__ void put_weight(const CachedArgs& a, float* weight, int b, int slot, float t, int add) {
   const long long place = cached_place(a.page_table + (size_t)b * a.max_pages, slot, a.page_size, a.pages);
   if (place < 0) { report_invalid(a.dev_status); return; }

@@ -7,8 +7,10 @@
 //   O^T [dh x N]      += V^T P^T      A = a tile of V, read along dh (its transpose costs nothing), B = P in shared memory
 // and no part of a tile is padding but the columns between the rows there are and the next of 16, 32, 64, 128.  The cache is read
 // once, by TMA, a page (or its largest power-of-two part) per copy, through a ring of four to ten tiles that runs ahead across work
-// items: bound by HBM up to 64 columns (one token of 131071 slots x 8 key heads x 128 in 89 us, 6.0 TB/s), by exponentials and
-// shared memory at 128.
+// items: bound by HBM up to 32 columns at head_dim 128 (one token of 131071 slots x 8 key heads in 89 us, 6.0 TB/s; eight blocks of 32
+// rows x 32 heads over up to 4288 slots 62 us of 54) and 16 at 64.  With more it is the softmax warps' way through a tile: the same with
+// 64 rows 79 us, with 128 rows 131, some 7000 cycles a tile of which exponentials are a seventh; 64 columns in a thread are more than
+// its 168 registers (312 bytes of spills at 128 columns, 72 at 64 x 128, 88 at 32 x 64).
 //
 // Softmax over the keys is a sum over lanes here.  A thread has one key's scores of all columns; the running maximum is only a
 // reference that has to lie within 2^8 of the true one (exact after the final division), so a tile costs one barrier that asks
