@@ -5,7 +5,8 @@
 ``PagedCache`` owns the pools, hands out pages and keeps the host's copy of the lengths (all sizes are known on the host, as
 everywhere in this package); every step of the path runs in the library's kernels.  Slots of a request are in no order that
 matters to attention; ``token`` holds the number that the caller gave a slot's token.  All work, the small uploads of table
-and lengths included, is enqueued on torch's current stream.
+and lengths included, is enqueued on torch's current stream; calls of one cache share a context, so those on different
+streams must not overlap.
 """
 from __future__ import annotations
 
